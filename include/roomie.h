@@ -11,6 +11,17 @@
  *   rm_place_optimal         optimal placement (accuracy   Sec. 6.4
  *                            baseline of Alg. 2)
  *
+ * and of the kernels of a served model's decode layer, the workload whose
+ * traces the predictor takes on this device:
+ *
+ *   rm_w4_linear             projection with 4-bit weights and group scales
+ *   rm_rotary_append         rotary positions, new tokens into an 8-bit cache
+ *   rm_cache_read            the values that pages of the cache hold
+ *   rm_cache_attention       attention over the cache
+ *   rm_norm_residual         gated, scaled residual between two norms
+ *   rm_trace_begin, _end     the launch shapes of these calls, as rm_occupancy
+ *                            takes them
+ *
  * Conventions shared by every entry point
  *  - Array arguments are DEVICE pointers (hipMalloc memory or the storage of a
  *    torch CUDA tensor), owned by the caller.  Struct arguments
@@ -25,7 +36,7 @@
  *    the caller's device int32 `status` word (RM_ST_* bits); pass a zeroed
  *    word to read them, or NULL to ignore them.  No C++ exception crosses
  *    this interface.
- *  - Floating point is IEEE fp64.  Occupancy, the prefix sums, aggregation
+ *  - The predictor's floating point is IEEE fp64.  Occupancy, the prefix sums, aggregation
  *    and placement evaluate the paper's expressions in sequential order
  *    without contraction, so they equal a plain sequential evaluation bit for
  *    bit.  The pair sweep weights each stretch through the reciprocal of
@@ -86,6 +97,11 @@ extern "C" {
                                         (never expected); the delays of that
                                         launch are not to be trusted           */
 
+#define RM_ST_BAD_LENGTH     1024    /* lengths or token_offsets out of range; the
+                                        sequence's tokens are skipped          */
+#define RM_ST_BAD_PAGE       2048    /* a page id outside [0, pages); the page is
+                                        neither written nor seen               */
+
 /* ---- limiter bits of rm_occupancy --------------------------------------- */
 #define RM_LIM_WARPS  1
 #define RM_LIM_REGS   2
@@ -103,6 +119,9 @@ extern "C" {
 #define RM_MAX_CAPACITY          8  /* capacity of rm_place                    */
 #define RM_MAX_OPT_MODELS       24  /* n_place of rm_place_optimal             */
 #define RM_MAX_OPT_CAPACITY      4  /* capacity of rm_place_optimal            */
+
+#define RM_MAX_NORM_WIDTH    32768  /* width of rm_norm_residual               */
+#define RM_MAX_SEQUENCES     65535  /* n_seqs of the cache calls               */
 
 /* Target-device descriptor: the SM limits of Eq. (1) and Eq. (2).
  * W = max_threads_per_sm / warp_size must be an integer <= 127, and the four
@@ -435,6 +454,175 @@ int rm_place_optimal(int32_t n_models, const double* delay, const double* iso_ti
                      int32_t n_devices, int32_t capacity, int32_t drop_mode, double* best_mean,
                      int32_t* best_device, void* workspace, size_t workspace_bytes,
                      int32_t* status, void* stream);
+
+/* ---- kernels of a decode layer ------------------------------------------- */
+
+/* Element type of activations, scales and gains. */
+#define RM_TYPE_BF16 0
+#define RM_TYPE_F16  1
+
+#define RM_ACT_NONE   0
+#define RM_ACT_SWIGLU 1  /* silu(first half of the outputs) * second half      */
+
+#define RM_NORM_RMS   0
+#define RM_NORM_LAYER 1
+
+#define RM_ROTARY_HALF        0  /* channel i turns with channel i + rot/2     */
+#define RM_ROTARY_INTERLEAVED 1  /* channel 2i turns with channel 2i + 1       */
+
+#define RM_CODES_INT8 0  /* two's complement, used range -127 .. 127           */
+#define RM_CODES_E4M3 1  /* fp8 e4m3 (finite, NaN 0x7f), largest 448           */
+
+/* A paged 8-bit cache.  A page holds page_tokens consecutive tokens of one
+ * sequence; for each kv head it has head_dim key codes a token (token by
+ * token), head_dim value codes a token (channel by channel: the tokens of a
+ * page are consecutive, as the product with the weights of a softmax reads
+ * them) and one scale for the keys and one for the values: a cached value is
+ * code * scale. */
+typedef struct {
+    void* k;              /* codes [n_pages][kv_heads][page_tokens][head_dim]  */
+    void* v;              /* codes [n_pages][kv_heads][head_dim][page_tokens]  */
+    float* k_scale;       /* [n_pages][kv_heads]                               */
+    float* v_scale;       /* [n_pages][kv_heads]                               */
+    int32_t n_pages;
+    int32_t kv_heads;
+    int32_t page_tokens;  /* 16, 32, 64 or 128                                 */
+    int32_t head_dim;     /* 64, 128 or 256                                    */
+    int32_t codes;        /* RM_CODES_*                                        */
+} rm_cache;
+
+/* Sequences of a call.  Sequence b's pages are table[b][0], table[b][1], ...;
+ * it holds lengths[b] tokens, the last n_b of which are the call's own, rows
+ * token_offsets[b] .. token_offsets[b+1]-1 of the token arrays.  Entries of
+ * the table behind the last page in use are not read. */
+typedef struct {
+    const int32_t* table;          /* [n_seqs][table_stride]                   */
+    const int32_t* lengths;        /* [n_seqs]                                 */
+    const int32_t* token_offsets;  /* [n_seqs + 1]; NULL: one token a sequence */
+    int32_t n_seqs;
+    int32_t table_stride;          /* pages that a row of the table can name   */
+    int32_t n_tokens;              /* rows of the token arrays                 */
+    int32_t max_tokens;            /* bound on n_b (host); a sequence with more
+                                      sets RM_ST_BAD_LENGTH and is skipped     */
+} rm_sequences;
+
+/*
+ * rm_w4_linear -- projection with 4-bit weights, for one to many rows:
+ *   t[m][j] = bias[j] + sum over i of
+ *             x[m][i] * scales[j][i/group] * (code[j][i] - zero[j][i/group])
+ *   y = t, or with RM_ACT_SWIGLU y[m][j] = silu(t[m][j]) * t[m][j + n/2].
+ * x: rows of k elements, x_stride apart.  codes: row j of k 4-bit codes at
+ *   codes + j*code_stride, element i in byte i/2, even elements in the low
+ *   half.  scales [n][ceil(k/group)]; zeros uint8 [n][ceil(k/group)], values
+ *   0..15 (NULL: 8 everywhere); bias [n] or NULL.  y: rows of n (SWIGLU: n/2)
+ *   elements, y_stride apart.  Sums are fp32, each output is rounded once.
+ *   An infinity in x gives NaN wherever its products meet.
+ * Errors: RM_EINVAL (NULL pointer, rows < 0, n or k < 1, a stride below its
+ *   row, group not a multiple of 32, SWIGLU with odd n, bad type or act),
+ *   RM_EUNSUPPORTED (a k over 2^24), RM_ELAUNCH.
+ */
+int rm_w4_linear(int32_t type, int32_t rows, int32_t n, int32_t k, const void* x,
+                 int64_t x_stride, const uint8_t* codes, int64_t code_stride, int32_t group,
+                 const void* scales, const uint8_t* zeros, const void* bias, int32_t act,
+                 void* y, int64_t y_stride, void* stream);
+
+/*
+ * rm_rotary_append -- turns the queries and keys of the call's tokens by their
+ * positions and appends keys and values to the cache:
+ *   (a, b) -> rot_scale * (a cos(p f) - b sin(p f), a sin(p f) + b cos(p f)),
+ * f = inv_freq[i] for pair i of `layout`, in the first `rot` channels of each
+ * head; the others are copied.  p = positions[token], or the token's index in
+ * its sequence where positions is NULL.  The angle is taken modulo one turn
+ * in fp64, so that long contexts lose nothing.
+ * q [n_tokens][heads][head_dim], k and v [n_tokens][kv_heads][head_dim]:
+ * strides in elements of tokens (q_stride ...) and heads (q_head_stride ...),
+ * channels consecutive.  q_out [n_tokens][heads][head_dim].
+ * A page and head that gets new tokens: scale = max(scale of its older tokens,
+ * largest new magnitude / Q), Q = 127 or 448; older codes become
+ * round(code * old scale / scale), new ones round(value / scale) (ties to
+ * even), and the slots behind the last token 0.  A non-finite value makes the page's scale, and so all that
+ * the head reads from the page, not finite.
+ * No page may be in two of the call's sequences where tokens are appended.
+ * heads may be 0 (q and q_out are then not read).
+ * Errors: RM_EINVAL (NULL pointer, negative size, rot odd or > head_dim, bad
+ *   type, layout or codes), RM_EUNSUPPORTED (page_tokens or head_dim not
+ *   listed, n_seqs over RM_MAX_SEQUENCES, heads or kv_heads over 65535),
+ *   RM_ELAUNCH.
+ */
+int rm_rotary_append(int32_t type, const rm_cache* cache, const rm_sequences* seqs,
+                     int32_t heads, const void* q, int64_t q_stride, int64_t q_head_stride,
+                     const void* k, int64_t k_stride, int64_t k_head_stride, const void* v,
+                     int64_t v_stride, int64_t v_head_stride, const int32_t* positions,
+                     const float* inv_freq, int32_t rot, int32_t layout, float rot_scale,
+                     void* q_out, int32_t* status, void* stream);
+
+/*
+ * rm_cache_read -- the keys and values that the pages pages[0..n) hold, as
+ * elements of `type`: k, v [n][page_tokens][kv_heads][head_dim].  A page id
+ * out of range gives zeros and RM_ST_BAD_PAGE.
+ * Errors: RM_EINVAL, RM_EUNSUPPORTED (as rm_rotary_append), RM_ELAUNCH.
+ */
+int rm_cache_read(int32_t type, const rm_cache* cache, int32_t n, const int32_t* pages, void* k,
+                  void* v, int32_t* status, void* stream);
+
+/*
+ * rm_cache_attention -- attention of the call's tokens over the cache:
+ *   out[t][h] = sum_j w_j value_j,  w = softmax over j of scale * q[t][h].key_j
+ * of kv head h / (heads / kv_heads), over the tokens j of t's sequence that it
+ * sees: j <= p, its own index, and, where window > 0, j > p - window.  A token
+ * that sees nothing (its sequence or a page is out of range) gets 0.
+ * q as in rm_rotary_append, out [n_tokens][heads][head_dim].  Logits, softmax
+ * statistics and sums are fp32; a cached code is exact in the product's type;
+ * the softmax weights enter the second product as f16 times the scale of the
+ * values' page, relative to the largest such scale so far.
+ * workspace: rm_cache_attention_workspace_bytes bytes, 256-byte aligned.
+ * Errors: RM_EINVAL (also heads not a multiple of kv_heads, scale not finite,
+ *   window < 0), RM_EUNSUPPORTED, RM_EWORKSPACE, RM_ELAUNCH.
+ */
+size_t rm_cache_attention_workspace_bytes(const rm_cache* cache, const rm_sequences* seqs,
+                                          int32_t heads);
+int rm_cache_attention(int32_t type, const rm_cache* cache, const rm_sequences* seqs,
+                       int32_t heads, const void* q, int64_t q_stride, int64_t q_head_stride,
+                       float scale, int32_t window, void* out, void* workspace,
+                       size_t workspace_bytes, int32_t* status, void* stream);
+
+/*
+ * rm_norm_residual -- the residual between two blocks and the norms around
+ * it, one pass:
+ *   u = y, or norm(y) * post_weight;   x' = x + alpha * gate * u;
+ *   n = norm(x') * pre_weight + pre_bias.
+ * norm is x / sqrt(mean(x^2) + eps) or (x - mean) / sqrt(variance + eps), in
+ * fp32 and of the unrounded x'.  Rows of `width` elements; x, y and gate with
+ * row strides in elements; gate_stride 0 is one row for all.  gate_width is
+ * `width`, or 1 for one gate a row.  Each of y (x' = x then), gate, post_weight
+ * (y then enters as it is), pre_weight, pre_bias may be NULL, and so may x_out
+ * or n_out, not both.  x_out may be x; outputs have rows of `width`.
+ * Errors: RM_EINVAL (NULL x, rows < 0, width < 1, a stride below its row, eps
+ *   or alpha not finite, gate or post_weight without y, bad type or kind),
+ *   RM_EUNSUPPORTED (width > RM_MAX_NORM_WIDTH), RM_ELAUNCH.
+ */
+int rm_norm_residual(int32_t type, int32_t kind, int32_t rows, int32_t width, const void* x,
+                     int64_t x_stride, const void* y, int64_t y_stride, const void* gate,
+                     int64_t gate_stride, int32_t gate_width, const void* post_weight,
+                     const void* pre_weight, const void* pre_bias, float alpha, float eps,
+                     void* x_out, void* n_out, void* stream);
+
+/* One launch as the predictor describes a kernel: blocks in the grid, threads
+ * a block, vector registers a thread, LDS bytes a block. */
+typedef struct {
+    int32_t grid, threads, regs, smem;
+} rm_launch;
+
+/*
+ * rm_trace_begin / rm_trace_end -- between them every launch of the calling
+ * thread's rm_w4_linear, rm_rotary_append, rm_cache_read, rm_cache_attention
+ * and rm_norm_residual calls is written to records[0..capacity) (host memory)
+ * in order; the launches themselves are as always.  rm_trace_end stores the
+ * number of launches, which may exceed the capacity, and ends the recording.
+ * Errors: RM_EINVAL (NULL, capacity < 0, begin in a recording, end outside).
+ */
+int rm_trace_begin(rm_launch* records, int32_t capacity);
+int rm_trace_end(int32_t* n_launches);
 
 /* Human-readable text for a return code; for RM_ELAUNCH it names the HIP
  * error of the calling thread's last failed call.  Never NULL. */

@@ -32,6 +32,8 @@ ST_BAD_EVENT = 64
 ST_INVALID_CONFIG = 128
 ST_BAD_DELAY = 256
 ST_WAIT_TIMEOUT = 512
+ST_BAD_LENGTH = 1024
+ST_BAD_PAGE = 2048
 
 ALIGN_NAMES = {"first": ALIGN_FIRST, "conflict_starts": ALIGN_CONFLICT_STARTS,
                "offsets": ALIGN_OFFSETS, "sampled_starts": ALIGN_SAMPLED_STARTS}
@@ -40,6 +42,12 @@ SWEEP_NAMES = {"temporal": SWEEP_TEMPORAL, "lockstep": SWEEP_LOCKSTEP,
                "adjusted": SWEEP_ADJUSTED}
 POLICY_EQUAL, POLICY_PRIORITY, POLICY_FCFS = 0, 1, 2
 POLICY_NAMES = {"equal": POLICY_EQUAL, "priority": POLICY_PRIORITY, "fcfs": POLICY_FCFS}
+
+TYPES = {torch.bfloat16: 0, torch.float16: 1}
+CODES = {torch.int8: 0, torch.float8_e4m3fn: 1}
+ACT_NAMES = {"none": 0, "swiglu": 1}
+NORM_NAMES = {"rms": 0, "layer": 1}
+ROTARY_NAMES = {"half": 0, "interleaved": 1}
 
 
 class DeviceDesc(ctypes.Structure):
@@ -60,6 +68,22 @@ class PairOpts(ctypes.Structure):
                 ("sweep_event_begin", ctypes.c_void_p), ("sweep_event_end", ctypes.c_void_p),
                 ("sweep_mode", ctypes.c_int32), ("start_draws", ctypes.c_void_p),
                 ("policy", ctypes.c_int32)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] +
+                [(n, ctypes.c_int32) for n in ("n_pages", "kv_heads", "page_tokens", "head_dim",
+                                               "codes")])
+
+
+class Sequences(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("table", "lengths", "token_offsets")] +
+                [(n, ctypes.c_int32) for n in ("n_seqs", "table_stride", "n_tokens",
+                                               "max_tokens")])
+
+
+class Launch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("grid", "threads", "regs", "smem")]
 
 
 _lib = None
@@ -94,6 +118,24 @@ def library():
         lib.rm_place_optimal.argtypes = [i32, P, P, P, i32, P, i32, i32, i32, P, P, P,
                                          ctypes.c_size_t, P, P]
         lib.rm_place_optimal.restype = ctypes.c_int
+        f32, sz = ctypes.c_float, ctypes.c_size_t
+        C, S = ctypes.POINTER(Cache), ctypes.POINTER(Sequences)
+        lib.rm_w4_linear.argtypes = [i32, i32, i32, i32, P, i64, P, i64, i32, P, P, P, i32, P,
+                                     i64, P]
+        lib.rm_rotary_append.argtypes = [i32, C, S, i32, P, i64, i64, P, i64, i64, P, i64, i64, P,
+                                         P, i32, i32, f32, P, P, P]
+        lib.rm_cache_read.argtypes = [i32, C, i32, P, P, P, P, P]
+        lib.rm_cache_attention_workspace_bytes.argtypes = [C, S, i32]
+        lib.rm_cache_attention_workspace_bytes.restype = sz
+        lib.rm_cache_attention.argtypes = [i32, C, S, i32, P, i64, i64, f32, i32, P, P, sz, P, P]
+        lib.rm_norm_residual.argtypes = [i32, i32, i32, i32, P, i64, P, i64, P, i64, i32, P, P, P,
+                                         f32, f32, P, P, P]
+        lib.rm_trace_begin.argtypes = [ctypes.POINTER(Launch), i32]
+        lib.rm_trace_end.argtypes = [ctypes.POINTER(i32)]
+        for f in (lib.rm_w4_linear, lib.rm_rotary_append, lib.rm_cache_read,
+                  lib.rm_cache_attention, lib.rm_norm_residual, lib.rm_trace_begin,
+                  lib.rm_trace_end):
+            f.restype = ctypes.c_int
         lib.rm_status_string.argtypes = [ctypes.c_int]
         lib.rm_status_string.restype = ctypes.c_char_p
         _lib = lib
@@ -365,3 +407,262 @@ def rm_place_optimal(delay, iso_time, kernel_count, models, n_devices, capacity,
     _check(code, "rm_place_optimal")
     out["workspace"] = workspace
     return out
+
+
+# ---- kernels of a decode layer ---------------------------------------------
+
+def _on_gpu(t, dtype, shape, name):
+    """Address of a contiguous GPU tensor of this type and shape; None for None."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous GPU tensor of {dtype} and shape "
+                         f"{tuple(shape)}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _rows(t, dtype, shape, name):
+    """Address and leading strides of a GPU tensor whose last axis is consecutive."""
+    if not t.is_cuda or t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name}: expected a GPU tensor of {dtype} and shape {tuple(shape)}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    strides = t.stride()
+    if strides[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{name}: the last axis must be consecutive")
+    return (t.data_ptr(),) + strides[:-1]
+
+
+def _pitch(stride, rows, width, name):
+    """Elements between rows; rows may not overlap."""
+    if rows <= 1:
+        return width
+    if stride < width:
+        raise ValueError(f"{name}: rows overlap")
+    return stride
+
+
+def _type_of(t, name):
+    code = TYPES.get(t.dtype)
+    if code is None or not t.is_cuda:
+        raise ValueError(f"{name}: expected a GPU tensor of bfloat16 or float16, got {t.dtype} "
+                         f"on {t.device}")
+    return code
+
+
+def _named(names, value, what):
+    code = names.get(value)
+    if code is None:
+        raise ValueError(f"{what}: expected one of {sorted(names)}, got {value!r}")
+    return code
+
+
+def _raw_stream(t):
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
+
+
+def new_cache(n_pages, kv_heads, page_tokens, head_dim, codes=torch.int8, device="cuda"):
+    """An empty paged 8-bit cache: codes int8 or float8_e4m3fn, one float32
+    scale for each page of tokens and head (include/roomie.h, rm_cache)."""
+    if codes not in CODES:
+        raise ValueError(f"codes: expected int8 or float8_e4m3fn, got {codes}")
+    shape = (n_pages, kv_heads)
+    return {"k": torch.zeros(shape + (page_tokens, head_dim), dtype=torch.uint8,
+                             device=device).view(codes),
+            "v": torch.zeros(shape + (head_dim, page_tokens), dtype=torch.uint8,
+                             device=device).view(codes),
+            "k_scale": torch.zeros(shape, dtype=torch.float32, device=device),
+            "v_scale": torch.zeros(shape, dtype=torch.float32, device=device)}
+
+
+def _cache_of(cache):
+    k = cache["k"]
+    if k.dim() != 4 or k.dtype not in CODES:
+        raise ValueError("cache: expected codes int8 or float8_e4m3fn [pages, kv_heads, "
+                         f"page_tokens, head_dim], got {k.dtype} {tuple(k.shape)}")
+    pages, heads, tokens, dim = k.shape
+    return Cache(_on_gpu(k, k.dtype, k.shape, "cache k"),
+                 _on_gpu(cache["v"], k.dtype, (pages, heads, dim, tokens), "cache v"),
+                 _on_gpu(cache["k_scale"], torch.float32, (pages, heads), "cache k_scale"),
+                 _on_gpu(cache["v_scale"], torch.float32, (pages, heads), "cache v_scale"),
+                 pages, heads, tokens, dim, CODES[k.dtype])
+
+
+def _sequences_of(table, lengths, token_offsets, n_tokens, max_tokens):
+    if table.dim() != 2:
+        raise ValueError("table: expected [sequences, pages]")
+    n, pages = table.shape
+    return Sequences(_on_gpu(table, torch.int32, (n, pages), "table"),
+                     _on_gpu(lengths, torch.int32, (n,), "lengths"),
+                     _on_gpu(token_offsets, torch.int32, (n + 1,), "token_offsets"),
+                     n, pages, n_tokens, max_tokens)
+
+
+def rm_w4_linear(x, codes, scales, group, zeros=None, bias=None, act="none", out=None):
+    """x [rows, k] through 4-bit weights: codes uint8 [n, ceil(k / 2)] (rows may
+    be strided), even elements in the low half; scales [n, ceil(k / group)] of
+    x's type; zeros uint8 like scales (None: 8); bias [n].  act "swiglu" takes
+    the first half of the outputs as gates of the second."""
+    kind = _type_of(x, "x")
+    if x.dim() != 2 or codes.dim() != 2:
+        raise ValueError("rm_w4_linear: expected x [rows, k] and codes [n, ceil(k / 2)]")
+    rows, k = x.shape
+    n = codes.shape[0]
+    if group < 1 or group % 32:
+        raise ValueError(f"group: expected a multiple of 32, got {group}")
+    groups = (n, -(-k // group))
+    act = _named(ACT_NAMES, act, "act")
+    if out is None:
+        out = torch.empty((rows, n // 2 if act else n), dtype=x.dtype, device=x.device)
+    xp, xs = _rows(x, x.dtype, x.shape, "x")
+    cp, cs = _rows(codes, torch.uint8, (n, (k + 1) // 2), "codes")
+    op, os_ = _rows(out, x.dtype, (rows, n // 2 if act else n), "out")
+    code = library().rm_w4_linear(
+        kind, rows, n, k, xp, _pitch(xs, rows, k, "x"), cp,
+        _pitch(cs, n, (k + 1) // 2, "codes"), group,
+        _on_gpu(scales, x.dtype, groups, "scales"), _on_gpu(zeros, torch.uint8, groups, "zeros"),
+        _on_gpu(bias, x.dtype, (n,), "bias"), act, op, _pitch(os_, rows, out.shape[1], "out"), _raw_stream(x))
+    if code:
+        _check(code, "rm_w4_linear")
+    return out
+
+
+def rm_rotary_append(q, k, v, inv_freq, cache, table, lengths, token_offsets=None, max_tokens=1,
+                     positions=None, layout="half", rot_scale=1.0, q_out=None, status=None):
+    """Turns q [tokens, heads, dim] and k [tokens, kv_heads, dim] by their
+    positions (2 * len(inv_freq) channels of each head, times rot_scale) and
+    appends k and v to the cache, whose `lengths` count the call's tokens
+    already.  q, k and v may be views of one projection.  Returns the turned
+    q (None for q None)."""
+    kind = _type_of(k, "k")
+    c = _cache_of(cache)
+    if k.dim() != 3:
+        raise ValueError("k: expected [tokens, kv_heads, head_dim]")
+    tokens, dim = k.shape[0], c.head_dim
+    s = _sequences_of(table, lengths, token_offsets, tokens, max_tokens)
+    kp, ks, kh = _rows(k, k.dtype, (tokens, c.kv_heads, dim), "k")
+    vp, vs, vh = _rows(v, k.dtype, (tokens, c.kv_heads, dim), "v")
+    heads, qp, qs, qh = 0, None, 0, 0
+    if q is not None:
+        if q.dim() != 3:
+            raise ValueError("q: expected [tokens, heads, head_dim]")
+        heads = q.shape[1]
+        qp, qs, qh = _rows(q, k.dtype, (tokens, heads, dim), "q")
+        if q_out is None:
+            q_out = torch.empty((tokens, heads, dim), dtype=k.dtype, device=k.device)
+    half = inv_freq.numel()
+    code = library().rm_rotary_append(
+        kind, c, s, heads, qp, qs, qh, kp, ks, kh, vp, vs, vh,
+        _on_gpu(positions, torch.int32, (tokens,), "positions"),
+        _on_gpu(inv_freq, torch.float32, (half,), "inv_freq"), 2 * half,
+        _named(ROTARY_NAMES, layout, "layout"), rot_scale,
+        _on_gpu(q_out, k.dtype, (tokens, heads, dim), "q_out"),
+        _on_gpu(status, torch.int32, (1,), "status"), _raw_stream(k))
+    if code:
+        _check(code, "rm_rotary_append")
+    return q_out
+
+
+def rm_cache_read(cache, pages, dtype=torch.bfloat16, status=None):
+    """Keys and values that `pages` (int32) hold: two tensors [pages,
+    page_tokens, kv_heads, head_dim]."""
+    c = _cache_of(cache)
+    n = pages.numel()
+    if dtype not in TYPES:
+        raise ValueError(f"dtype: expected bfloat16 or float16, got {dtype}")
+    k, v = (torch.empty((n, c.page_tokens, c.kv_heads, c.head_dim), dtype=dtype,
+                        device=pages.device) for _ in range(2))
+    code = library().rm_cache_read(TYPES[dtype], c, n,
+                                   _on_gpu(pages, torch.int32, (n,), "pages"), k.data_ptr(),
+                                   v.data_ptr(), _on_gpu(status, torch.int32, (1,), "status"),
+                                   _raw_stream(pages))
+    if code:
+        _check(code, "rm_cache_read")
+    return k, v
+
+
+def rm_cache_attention(q, cache, table, lengths, token_offsets=None, max_tokens=1, scale=None,
+                       window=0, workspace=None, out=None, status=None):
+    """Attention of q [tokens, heads, dim] over the cache (causal; `window` > 0
+    keeps each token's last `window`).  scale None: 1 / sqrt(dim)."""
+    kind = _type_of(q, "q")
+    c = _cache_of(cache)
+    if q.dim() != 3:
+        raise ValueError("q: expected [tokens, heads, head_dim]")
+    tokens, heads = q.shape[0], q.shape[1]
+    shape = (tokens, heads, c.head_dim)
+    qp, qs, qh = _rows(q, q.dtype, shape, "q")
+    s = _sequences_of(table, lengths, token_offsets, tokens, max_tokens)
+    lib = library()
+    if workspace is None:
+        need = lib.rm_cache_attention_workspace_bytes(c, s, heads)
+        if need == 0:
+            raise ValueError("rm_cache_attention: invalid sizes or options")
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    if out is None:
+        out = torch.empty(shape, dtype=q.dtype, device=q.device)
+    code = lib.rm_cache_attention(
+        kind, c, s, heads, qp, qs, qh, c.head_dim ** -0.5 if scale is None else scale, window,
+        _on_gpu(out, q.dtype, shape, "out"), workspace.data_ptr(), workspace.numel(),
+        _on_gpu(status, torch.int32, (1,), "status"), _raw_stream(q))
+    if code:
+        _check(code, "rm_cache_attention")
+    return out
+
+
+def rm_norm_residual(x, y=None, gate=None, post_weight=None, pre_weight=None, pre_bias=None,
+                     kind="rms", alpha=1.0, eps=1e-6, x_out=None, n_out=None):
+    """(x', n): x' = x + alpha * gate * y, y normalised and times post_weight
+    where that is given; n = x' normalised times pre_weight plus pre_bias.
+    x, y [rows, width]; gate [width], [rows, 1] or [rows, width].  Without y
+    x' is x itself."""
+    code_type = _type_of(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x: expected [rows, width]")
+    rows, width = shape = x.shape
+    xp, xs = _rows(x, x.dtype, shape, "x")
+    yp, ys = _rows(y, x.dtype, shape, "y") if y is not None else (None, 0)
+    gp, gs, gw = None, 0, 0
+    if gate is not None:
+        if gate.dim() == 1:
+            gp, gw = _on_gpu(gate, x.dtype, (width,), "gate"), width
+        else:
+            gw = gate.shape[1]
+            gp, gs = _rows(gate, x.dtype, (rows, gw), "gate")
+            gs = gs if rows > 1 else 0
+    if x_out is None:
+        x_out = x if y is None else torch.empty(shape, dtype=x.dtype, device=x.device)
+    if n_out is None:
+        n_out = torch.empty(shape, dtype=x.dtype, device=x.device)
+    code = library().rm_norm_residual(
+        code_type, _named(NORM_NAMES, kind, "kind"), rows, width, xp,
+        _pitch(xs, rows, width, "x"), yp, _pitch(ys, rows, width, "y") if yp else 0, gp,
+        gs, gw, _on_gpu(post_weight, x.dtype, (width,), "post_weight"),
+        _on_gpu(pre_weight, x.dtype, (width,), "pre_weight"),
+        _on_gpu(pre_bias, x.dtype, (width,), "pre_bias"), alpha, eps,
+        None if x_out is x and y is None else _on_gpu(x_out, x.dtype, shape, "x_out"),
+        _on_gpu(n_out, x.dtype, shape, "n_out"), _raw_stream(x))
+    if code:
+        _check(code, "rm_norm_residual")
+    return x_out, n_out
+
+
+class rm_trace:
+    """Context manager: the launch shapes of the decode-layer calls inside it,
+    as a list of dicts `launches` (grid, threads, regs, smem) after it."""
+
+    def __init__(self, capacity=4096):
+        self._records = (Launch * capacity)()
+        self.launches = []
+
+    def __enter__(self):
+        _check(library().rm_trace_begin(self._records, len(self._records)), "rm_trace_begin")
+        return self
+
+    def __exit__(self, *exc):
+        n = ctypes.c_int32()
+        _check(library().rm_trace_end(ctypes.byref(n)), "rm_trace_end")
+        if n.value > len(self._records) and exc[0] is None:
+            raise RuntimeError(f"rm_trace: {n.value} launches, room for {len(self._records)}")
+        self.launches = [{f: getattr(r, f) for f, _ in Launch._fields_}
+                         for r in self._records[:min(n.value, len(self._records))]]
+        return False

@@ -8,16 +8,23 @@
 
 #include "rm_common.h"
 
-namespace {
+static thread_local char g_last_hip_error[160] = "";
 
-thread_local char g_last_hip_error[160] = "";
+namespace rm {
 
+// Keeps the error's name for rm_status_string.
 int launch_failed(hipError_t e)
 {
     std::snprintf(g_last_hip_error, sizeof g_last_hip_error, "%s: %s", hipGetErrorName(e),
                   hipGetErrorString(e));
     return RM_ELAUNCH;
 }
+
+}  // namespace rm
+
+namespace {
+
+using rm::launch_failed;
 
 bool desc_ok(const rm_device_desc* d)
 {

@@ -1,0 +1,463 @@
+// attend.hip -- attention over the paged 8-bit cache (rm_cache_attention).
+//
+// The rows of a tile are the (token, query head) pairs that share a kv head,
+// tokens first: 16 for a decode step, up to 64 for a chunk of a prompt.  A wave
+// takes 64 cached tokens at a time, all in registers, with the running maximum
+// and sum of the softmax:
+//   S^T = K Q^T   v_mfma_f32_16x16x32 in q's type, keys as the 16 rows
+//   O^T += V^T P  the same in f16, value channels as the 16 rows
+// Which token a row of the first product stands for is free, so row i of
+// instruction t is token (i / 4) * 16 + 4 t + i % 4: a lane then ends up with the
+// weights of 16 neighbouring tokens, exactly the operand that the second
+// product wants from it, and with values stored channel by channel its other
+// operand is one 16-byte load.  Nothing passes through LDS until the waves join.
+//
+// Codes are exact in bf16 and f16.  Scales are constant over a page, so they
+// multiply the logits and, relative to the largest so far, the weights.
+//
+// A step of decoding is bound by reading the codes once.  The token axis is
+// split over the workgroup's waves and, when there are few tiles, over
+// workgroups whose partial results a second kernel joins.
+#include "rm_common.h"
+#include "rm_decode.h"
+
+namespace rm {
+namespace {
+
+constexpr int kBlock = 64;    // cached tokens a wave takes at a time
+constexpr int kWaves = 4;
+
+__device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ inline f32x4 mfma(f16x8 a, f16x8 b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// Eight codes as elements of the product's type; exact.
+template <int FMT>
+__device__ inline void decode8(uint32_t lo, uint32_t hi, bf16x8& out)
+{
+    if (FMT == RM_CODES_E4M3) {
+        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
+        const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
+        const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
+        const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+        out = bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            out[i] = (bf16)(float)(int8_t)(lo >> (8 * i));
+            out[4 + i] = (bf16)(float)(int8_t)(hi >> (8 * i));
+        }
+    }
+}
+template <int FMT>
+__device__ inline void decode8(uint32_t lo, uint32_t hi, f16x8& out)
+{
+    if (FMT == RM_CODES_E4M3) {
+        const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false);
+        const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
+        const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false);
+        const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
+        out = f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    } else {
+        // code + 128 in the low bits of 1024 is 1152 + code; the difference is exact
+        const uint32_t w[2] = {lo ^ 0x80808080u, hi ^ 0x80808080u};
+        u32x4 r;
+        const f16x2 c = {(f16)1152.0f, (f16)1152.0f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t p = __builtin_amdgcn_perm(0x64646464u, w[i >> 1],
+                                                     i & 1 ? 0x04030402u : 0x04010400u);
+            r[i] = __builtin_bit_cast(uint32_t, (f16x2)(__builtin_bit_cast(f16x2, p) - c));
+        }
+        out = __builtin_bit_cast(f16x8, r);
+    }
+}
+
+// 2^x; results below the normal range are 0.
+__device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+struct Plan {
+    int32_t tiles, splits;      // tiles of rows a sequence and kv head; splits of a tile
+};
+
+// Rows and token range of a tile.
+struct Tile {
+    int32_t rows, first_pos, lo, hi, all_lo, all_hi;
+};
+
+__device__ inline Tile tile_of(const Sequence& s, int32_t group, int32_t window, int32_t tile,
+                               int32_t height)
+{
+    Tile t;
+    const int32_t r0 = tile * height;
+    t.rows = min(height, s.n * group - r0);
+    t.first_pos = s.length - s.n;
+    const int32_t p0 = t.first_pos + r0 / group, p1 = t.first_pos + (r0 + t.rows - 1) / group;
+    t.lo = window > 0 ? max(0, p0 - window + 1) : 0;        // seen by some row
+    t.hi = p1 + 1;
+    t.all_lo = window > 0 ? max(0, p1 - window + 1) : 0;    // seen by every row
+    t.all_hi = p0 + 1;
+    return t;
+}
+
+template <typename T, int FMT, int D, int C>
+__global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a, Plan plan)
+{
+    typedef typename Vec<T>::x8 V;
+    constexpr int H = 16 * C;                  // rows of a tile
+    constexpr int PITCH = D + 4;
+    __shared__ float join[H * PITCH];
+    __shared__ float join_m[kWaves][H], join_l[kWaves][H], join_s[kWaves];
+
+    const int KV = a.cache.kv_heads, TK = a.cache.page_tokens, G = a.heads / KV;
+    int64_t at = blockIdx.x;
+    const int split = (int)(at % plan.splits);
+    at /= plan.splits;
+    const int tile = (int)(at % plan.tiles);
+    at /= plan.tiles;
+    const int head = (int)(at % KV), b = (int)(at / KV);
+    const Sequence s = sequence_of(a.seqs, TK, b);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, quad = lane >> 4;
+
+    if (s.n == 0) {
+        // no token, or one of a sequence that is out of range: zeros
+        if (s.bad && a.status && threadIdx.x == 0) atomicOr(a.status, RM_ST_BAD_LENGTH);
+        if (tile || split) return;
+        int64_t from = b, upto = (int64_t)b + 1;
+        if (a.seqs.token_offsets) from = s.first, upto = a.seqs.token_offsets[b + 1];
+        if (from < 0 || upto > a.seqs.n_tokens) return;
+        for (int64_t t = from; t < upto; ++t)
+            for (int i = threadIdx.x; i < G * D; i += kWaves * 64)
+                static_cast<T*>(a.out)[(t * a.heads + head * G) * D + i] = (T)0.0f;
+        return;
+    }
+    if (tile * H >= s.n * G) return;
+    const Tile t = tile_of(s, G, a.window, tile, H);
+    const int b0 = t.lo / kBlock, b1 = (t.hi + kBlock - 1) / kBlock;
+    const int per = (b1 - b0 + plan.splits - 1) / plan.splits;
+    const int from = b0 + split * per, upto = min(b1, from + per);
+
+    // queries: row 16 c + li of the tile, channels 64 j + 16 quad + 8 k of the
+    // operand for the k-th half of the j-th 16-byte load of keys
+    V q[C][D / 32];
+    int32_t pos[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int r = tile * H + min(c * 16 + li, t.rows - 1);
+        pos[c] = t.first_pos + r / G;
+        const T* row = static_cast<const T*>(a.q) + (s.first + r / G) * a.q_stride +
+                       (head * G + r % G) * a.q_head;
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k)
+            q[c][k] = load8(row + (k >> 1) * 64 + quad * 16 + (k & 1) * 8);
+    }
+
+    f32x4 o[D / 16][C];
+    float m[C], l[C], ref = 0.0f;              // ref: largest scale of values so far
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        m[c] = -INFINITY;
+        l[c] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) o[d][c] = f32x4{0, 0, 0, 0};
+    }
+    const int32_t* table = a.seqs.table + (int64_t)b * a.seqs.table_stride;
+    const int shift = __ffs(TK) - 1, last_page = (s.length - 1) >> shift;
+    const float to_log2 = a.scale * 1.44269504088896340736f;
+    int32_t st = 0;
+
+    for (int block = from + wave; block < upto; block += kWaves) {
+        const int t0 = block * kBlock;
+        // the pages of the 16 tokens whose keys and whose values the lane loads
+        const int tk = t0 + (li >> 2) * 16, tv = t0 + quad * 16;
+        int32_t pk = table[min(tk >> shift, last_page)], pv = table[min(tv >> shift, last_page)];
+        const bool bad = pv < 0 || pv >= a.cache.n_pages;
+        if (bad) st = RM_ST_BAD_PAGE, pv = 0;
+        if (pk < 0 || pk >= a.cache.n_pages) pk = 0;
+        const int64_t bk = (int64_t)pk * KV + head, bv = (int64_t)pv * KV + head;
+        const uint8_t* kp = static_cast<const uint8_t*>(a.cache.k) +
+                            (bk * TK + (tk & (TK - 1)) + (li & 3)) * D + quad * 16;
+        const uint8_t* vp = static_cast<const uint8_t*>(a.cache.v) + (bv * D + li) * TK + (tv & (TK - 1));
+        u32x4 kc[4][D / 64], vc[D / 16];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j)
+                kc[i][j] = *reinterpret_cast<const u32x4*>(kp + i * 4 * D + j * 64);
+        const float ks = a.cache.k_scale[bv] * to_log2;
+        const float vs = a.cache.v_scale[bv];
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d)
+            vc[d] = *reinterpret_cast<const u32x4*>(vp + d * 16 * TK);
+
+        f32x4 sc[4][C];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) sc[i][c] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) {
+                V e;
+                decode8<FMT>(kc[i][k >> 1][(k & 1) * 2], kc[i][k >> 1][(k & 1) * 2 + 1], e);
+#pragma unroll
+                for (int c = 0; c < C; ++c) sc[i][c] = mfma(e, q[c][k], sc[i][c]);
+            }
+        }
+        const bool whole = t0 >= t.all_lo && t0 + kBlock <= t.all_hi && !__any(bad);
+        float top[C];
+        bool moved = false;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            float x = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float v = sc[i][c][k] * ks;
+                    if (!whole) {
+                        const int token = tv + 4 * i + k;
+                        const bool seen = token <= pos[c] && !bad &&
+                                          (a.window <= 0 || token > pos[c] - a.window);
+                        v = seen ? v : -INFINITY;
+                    }
+                    sc[i][c][k] = v;
+                    x = fmaxf(x, v);
+                }
+            top[c] = fmaxf(m[c], rows_reduce<Max>(x));
+            moved |= top[c] > m[c];
+        }
+        const float now = fmaxf(ref, rows_reduce<Max>(bad ? 0.0f : vs));
+        if (__any(moved || now > ref)) {
+            const float shrink = now > 0.0f ? ref / now : 1.0f;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const float f = top[c] == -INFINITY ? 1.0f : exp2_of(m[c] - top[c]);
+                l[c] *= f;
+                m[c] = top[c];
+#pragma unroll
+                for (int d = 0; d < D / 16; ++d) o[d][c] *= f * shrink;
+            }
+            ref = now;
+        }
+        const float share = ref > 0.0f ? vs / ref : 0.0f;
+        f16x8 p[2][C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const float base = m[c] == -INFINITY ? 0.0f : m[c];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float e = exp2_of(sc[i][c][k] - base);
+                    l[c] += e;
+                    float w = e * share;
+                    if (!whole) w = e == 0.0f ? 0.0f : w;
+                    p[i >> 1][c][(i & 1) * 4 + k] = (f16)w;
+                }
+        }
+        if (!whole) {
+            // bytes of tokens that no row sees, which may hold anything
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const bool keep = tv + i >= t.lo && tv + i < t.hi && !bad;
+                const uint32_t mask = keep ? ~0u : ~(255u << (8 * (i & 3)));
+#pragma unroll
+                for (int d = 0; d < D / 16; ++d) vc[d][i >> 2] &= mask;
+            }
+        }
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                f16x8 e;
+                decode8<FMT>(vc[d][2 * k], vc[d][2 * k + 1], e);
+#pragma unroll
+                for (int c = 0; c < C; ++c) o[d][c] = mfma(e, p[k][c], o[d][c]);
+            }
+    }
+    report_status(a.status, st);
+
+    // join the waves: common maximum, then the sums one wave after the other
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        l[c] = rows_reduce<Add>(l[c]);
+        if (quad == 0) join_m[wave][c * 16 + li] = m[c], join_l[wave][c * 16 + li] = l[c];
+    }
+    __syncthreads();
+    float f[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        float top = join_m[0][c * 16 + li];
+        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, join_m[w][c * 16 + li]);
+        f[c] = exp2_of(m[c] - (top == -INFINITY ? 0.0f : top)) * ref;
+    }
+    for (int w = 0; w < kWaves; ++w) {
+        if (wave == w) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int d = 0; d < D / 16; ++d) {
+                    f32x4* to = reinterpret_cast<f32x4*>(
+                        &join[(c * 16 + li) * PITCH + d * 16 + quad * 4]);
+                    const f32x4 mine = o[d][c] * f[c];
+                    *to = w == 0 ? mine : *to + mine;
+                }
+        }
+        __syncthreads();
+    }
+    float* part = static_cast<float*>(a.workspace);
+    const int64_t n_parts = (int64_t)gridDim.x;
+    for (int u = threadIdx.x; u < t.rows * (D / 8); u += kWaves * 64) {
+        const int row = u / (D / 8), d = u % (D / 8) * 8;
+        float top = join_m[0][row];
+        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, join_m[w][row]);
+        const float base = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f;
+        for (int w = 0; w < kWaves; ++w) sum += join_l[w][row] * exp2_of(join_m[w][row] - base);
+        const float* from_row = &join[row * PITCH + d];
+        if (plan.splits == 1) {
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            V r;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r[i] = (T)(from_row[i] * inv);
+            const int rr = tile * H + row;
+            store8(static_cast<T*>(a.out) +
+                       ((int64_t)(s.first + rr / G) * a.heads + head * G + rr % G) * D + d, r);
+        } else {
+            float* to = part + ((int64_t)blockIdx.x * H + row) * D + d;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) to[i] = from_row[i];
+            if (d == 0) {
+                float* ml = part + n_parts * H * D + ((int64_t)blockIdx.x * H + row) * 2;
+                ml[0] = top;
+                ml[1] = sum;
+            }
+        }
+    }
+}
+
+// One wave a row of a tile: the splits' partial results, in order.
+template <typename T, int D, int C>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, Plan plan, int64_t n_parts)
+{
+    constexpr int H = 16 * C;
+    const int KV = a.cache.kv_heads, G = a.heads / KV;
+    const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 6;
+    const int lane = threadIdx.x & 63;
+    int64_t at = unit;
+    const int row = (int)(at % H);
+    at /= H;
+    const int64_t block = at * plan.splits;
+    const int tile = (int)(at % plan.tiles);
+    at /= plan.tiles;
+    const int head = (int)(at % KV);
+    if (at / KV >= a.seqs.n_seqs) return;
+    const Sequence s = sequence_of(a.seqs, a.cache.page_tokens, (int)(at / KV));
+    const int rr = tile * H + row;
+    if (rr >= s.n * G) return;
+    const float* part = static_cast<const float*>(a.workspace);
+    const float* ml = part + n_parts * H * D + (block * H + row) * 2;
+    float top = -INFINITY;
+    for (int i = 0; i < plan.splits; ++i) top = fmaxf(top, ml[(int64_t)i * H * 2]);
+    const float base = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f, v[D / 64];
+#pragma unroll
+    for (int k = 0; k < D / 64; ++k) v[k] = 0.0f;
+    for (int i = 0; i < plan.splits; ++i) {
+        const float li = ml[(int64_t)i * H * 2 + 1];
+        if (li == 0.0f) continue;                   // saw nothing
+        const float f = exp2_of(ml[(int64_t)i * H * 2] - base);
+        sum = __builtin_fmaf(li, f, sum);
+        const float* from = part + ((block + i) * H + row) * D;
+#pragma unroll
+        for (int k = 0; k < D / 64; ++k) v[k] = __builtin_fmaf(from[k * 64 + lane], f, v[k]);
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    T* out = static_cast<T*>(a.out) +
+             ((int64_t)(s.first + rr / G) * a.heads + head * G + rr % G) * D;
+#pragma unroll
+    for (int k = 0; k < D / 64; ++k) out[k * 64 + lane] = (T)(v[k] * inv);
+}
+
+int columns_of(int32_t head_dim, int64_t rows)
+{
+    if (rows <= 16) return 1;
+    if (rows <= 32 || head_dim > 128) return 2;
+    return 4;
+}
+
+Plan plan_of(const rm_cache& c, const rm_sequences& s, int32_t heads)
+{
+    const int64_t rows = (int64_t)s.max_tokens * (heads / c.kv_heads);
+    const int height = 16 * columns_of(c.head_dim, rows);
+    Plan p;
+    p.tiles = (int32_t)((rows + height - 1) / height);
+    const int64_t units = (int64_t)s.n_seqs * c.kv_heads * p.tiles;
+    // two workgroups a CU where the tokens reach: a wave has one block at least
+    const int64_t blocks = ((int64_t)s.table_stride * c.page_tokens + kBlock - 1) / kBlock;
+    const int64_t want = units > 0 ? (2 * kComputeUnits + units - 1) / units : 1;
+    const int64_t most = (blocks + kWaves - 1) / kWaves;
+    p.splits = (int32_t)(want < most ? want : most);
+    if (p.splits < 1) p.splits = 1;
+    return p;
+}
+
+template <typename T, int FMT, int D, int C>
+hipError_t launch_columns(const AttendArgs& a, const Plan& p, hipStream_t s)
+{
+    const int64_t units = (int64_t)a.seqs.n_seqs * a.cache.kv_heads * p.tiles;
+    const int64_t parts = units * p.splits;
+    if (parts == 0) return hipSuccess;
+    if (parts > 0x7fffffff) return hipErrorInvalidValue;
+    hipError_t e = launch(attend_kernel<T, FMT, D, C>, dim3((unsigned)parts), kWaves * 64, 0, s,
+                          a, p);
+    if (e != hipSuccess || p.splits == 1) return e;
+    return launch(attend_join_kernel<T, D, C>, dim3((unsigned)(units * 16 * C / 4)), 256, 0, s, a,
+                  p, parts);
+}
+
+template <typename T, int FMT, int D>
+hipError_t launch_dim(const AttendArgs& a, hipStream_t s)
+{
+    const Plan p = plan_of(a.cache, a.seqs, a.heads);
+    const int c = columns_of(D, (int64_t)a.seqs.max_tokens * (a.heads / a.cache.kv_heads));
+    if (c == 1) return launch_columns<T, FMT, D, 1>(a, p, s);
+    if (c == 2) return launch_columns<T, FMT, D, 2>(a, p, s);
+    if constexpr (D <= 128) return launch_columns<T, FMT, D, 4>(a, p, s);
+    return hipErrorInvalidValue;
+}
+
+template <typename T, int FMT>
+hipError_t launch_codes(const AttendArgs& a, hipStream_t s)
+{
+    if (a.cache.head_dim == 64) return launch_dim<T, FMT, 64>(a, s);
+    if (a.cache.head_dim == 128) return launch_dim<T, FMT, 128>(a, s);
+    return launch_dim<T, FMT, 256>(a, s);
+}
+
+}  // namespace
+
+size_t attend_workspace(const rm_cache& c, const rm_sequences& s, int32_t heads)
+{
+    const Plan p = plan_of(c, s, heads);
+    if (p.splits == 1) return 256;
+    const int height = 16 * columns_of(c.head_dim, (int64_t)s.max_tokens * (heads / c.kv_heads));
+    const size_t parts = (size_t)s.n_seqs * c.kv_heads * p.tiles * p.splits;
+    return (parts * height * (c.head_dim + 2) * sizeof(float) + 255) / 256 * 256;
+}
+
+hipError_t launch_attend(int type, const AttendArgs& a, hipStream_t s)
+{
+    if (type == RM_TYPE_BF16)
+        return a.cache.codes == RM_CODES_INT8 ? launch_codes<bf16, RM_CODES_INT8>(a, s)
+                                              : launch_codes<bf16, RM_CODES_E4M3>(a, s);
+    return a.cache.codes == RM_CODES_INT8 ? launch_codes<f16, RM_CODES_INT8>(a, s)
+                                          : launch_codes<f16, RM_CODES_E4M3>(a, s);
+}
+
+}  // namespace rm

@@ -1,0 +1,252 @@
+"""rm_rotary_append and rm_cache_read against their 64-bit definitions.
+
+A stored code may differ from the exact quotient by half a step, plus what fp32
+scale and quotient lose of it: some 4 roundings, 2^-20 of the quotient with
+room to spare.  A turned key is a difference of two products, so it is off by a
+few roundings of the pair and not of the result: 2^-21 of the largest
+magnitude, and the page's largest code stands for that."""
+import pytest
+import torch
+
+import decode_ref as ref
+from decode_common import make_cache, offsets_of
+from paper_2607_16784_amd import api
+
+pytestmark = pytest.mark.gpu
+INT8, E4M3 = torch.int8, torch.float8_e4m3fn
+
+
+def step_of(q, codes):
+    if codes == INT8:
+        return torch.ones_like(q)
+    e = torch.floor(torch.log2(q.abs().clamp(min=2.0 ** -6)))
+    return torch.exp2(e - 3)
+
+
+def check_cache(cache, after, what=("k", "v")):
+    for name in what:
+        got = ref.codes_f64(cache[name])
+        got = got if name == "k" else got.transpose(2, 3)
+        q = after[name]
+        tol = step_of(q, cache[name].dtype) * 0.5 + q.abs() * 2.0 ** -20 + 1e-12
+        if name == "k":
+            tol = tol + ref.LARGEST[cache[name].dtype] * 2.0 ** -21
+        err = (got - q).abs()
+        assert torch.all(err <= tol), f"{name}: worst {float((err / tol).max())}"
+        s, want = ref.f64(cache[name + "_scale"]), after[name + "_scale"]
+        assert torch.all((s - want).abs() <= want * 2.0 ** -20), name + " scale"
+
+
+def frequencies(rot, base=10000.0):
+    return torch.tensor([base ** (-2 * i / rot) for i in range(rot // 2)], dtype=torch.float32)
+
+
+def run(lengths, new, heads, kv, page, dim, codes, dtype, rot, layout, seed, positions=None,
+        big=1.0, scale=1.25):
+    cache, table, lens, _ = make_cache(lengths, kv, page, dim, codes, seed)
+    g = torch.Generator().manual_seed(seed + 1)
+    off = offsets_of(new)
+    # one fused projection: q, k and v are views of it
+    fused = (torch.randn((off[-1], heads + 2 * kv, dim), generator=g) * big).to(dtype).cuda()
+    q, k, v = fused[:, :heads], fused[:, heads:heads + kv], fused[:, heads + kv:]
+    inv = frequencies(rot) if rot else torch.zeros(0)
+    pos = positions
+    if pos is None:
+        pos = [n - w + i for n, w in zip(lengths, new) for i in range(w)]
+    turned_k = ref.rotate(k, pos, inv, layout, scale)
+    after = ref.append(cache, table, lengths, off, turned_k, ref.f64(v))
+    st = api.new_status()
+    got = api.rm_rotary_append(
+        q, k, v, inv.cuda(), cache, table, lens,
+        token_offsets=torch.tensor(off, dtype=torch.int32).cuda(), max_tokens=max(new + [1]),
+        positions=None if positions is None else torch.tensor(positions,
+                                                              dtype=torch.int32).cuda(),
+        layout=layout, rot_scale=scale, status=st)
+    assert int(st.item()) == 0
+    want = ref.rotate(q, pos, inv, layout, scale)
+    err = (ref.f64(got) - want).abs()
+    size = ref.f64(q).abs().amax(dim=2, keepdim=True) * scale
+    assert torch.all(err <= ref.ROUND[dtype] * want.abs() + 2.0 ** -20 * size + 1e-9)
+    check_cache(cache, after)
+    return cache, table, after
+
+
+CASES = [
+    # lengths, new, heads, kv, page, dim, rot
+    ([1], [1], 1, 1, 16, 64, 64),
+    ([17, 1, 16], [1, 1, 1], 4, 2, 16, 128, 128),
+    ([40, 5, 64], [7, 5, 0], 3, 1, 32, 64, 32),
+    ([130, 64, 63, 65], [130, 1, 2, 65], 5, 5, 64, 128, 64),
+    ([300], [137], 8, 2, 128, 256, 256),
+    ([200, 33], [1, 33], 2, 2, 128, 64, 10),
+    ([31, 90], [3, 20], 4, 4, 16, 256, 250),
+    ([90], [60], 2, 1, 64, 128, 0),
+    ([16, 16, 32], [16, 1, 17], 0, 3, 16, 64, 64),
+]
+
+
+@pytest.mark.parametrize("codes", [INT8, E4M3], ids=["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_against_64_bits(case, layout, dtype, codes):
+    lengths, new, heads, kv, page, dim, rot = CASES[case]
+    run(lengths, new, max(heads, 1), kv, page, dim, codes, dtype, rot, layout, seed=case)
+
+
+def test_without_queries():
+    cache, table, lens, _ = make_cache([20], 2, 16, 64, INT8, 3)
+    other = {n: t.clone() for n, t in cache.items()}
+    k, v = (torch.randn((1, 2, 64), device="cuda").bfloat16() for _ in range(2))
+    inv = frequencies(64).cuda()
+    assert api.rm_rotary_append(None, k, v, inv, cache, table, lens) is None
+    api.rm_rotary_append(k, k, v, inv, other, table, lens)
+    for n in cache:
+        assert torch.equal(cache[n].view(torch.uint8), other[n].view(torch.uint8)), n
+
+
+def test_a_louder_token_rescales_the_page_and_a_quieter_one_does_not():
+    for big in (0.01, 30.0):
+        cache, _, _ = run([30, 18], [1, 2], 2, 2, 32, 64, INT8, torch.bfloat16, 64, "half",
+                          seed=21, big=big)
+        assert torch.all(torch.isfinite(cache["k_scale"]))
+
+
+def test_tokens_one_at_a_time_and_all_zero():
+    # a page filled by 16 calls, the first with zeros: its scale is 0
+    cache = api.new_cache(1, 1, 16, 64)
+    table = torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+    inv = frequencies(64).cuda()
+    rows = []
+    for n in range(1, 17):
+        x = torch.randn((1, 1, 64), device="cuda").half() * (n - 1)
+        rows.append(x)
+        lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+        api.rm_rotary_append(None, x, x, inv, cache, table, lens)
+        if n == 1:
+            assert float(cache["v_scale"][0, 0]) == 0.0
+        _, v = api.rm_cache_read(cache, table.reshape(-1), torch.float16)
+        top = max(float(r.abs().max()) for r in rows)
+        # each raise of the scale may move an older code by half a step more
+        assert float((v[0, :n, 0].float() - torch.cat(rows)[:, 0].float()).abs().max()) <= \
+            top / 127 * (0.5 + 0.5 * n)
+        assert torch.all(v[0, n:] == 0)
+
+
+def test_positions_beyond_a_million_keep_their_angle():
+    pos = [0, 1, 65535, 1000003, 2 ** 31 - 1]
+    run([5], [5], 2, 1, 16, 64, INT8, torch.float16, 64, "half", seed=31, positions=pos)
+
+
+def test_pages_beyond_4_gib():
+    # codes of the last page start behind 2^32 bytes
+    kv, page, dim = 8, 128, 256
+    pages = 2 ** 32 // (kv * page * dim) + 3
+    cache = {"k": torch.empty((pages, kv, page, dim), dtype=INT8, device="cuda"),
+             "v": torch.empty((pages, kv, dim, page), dtype=INT8, device="cuda"),
+             "k_scale": torch.zeros((pages, kv), device="cuda"),
+             "v_scale": torch.zeros((pages, kv), device="cuda")}
+    table = torch.tensor([[pages - 1]], dtype=torch.int32, device="cuda")
+    lens = torch.tensor([3], dtype=torch.int32, device="cuda")
+    off = torch.tensor([0, 3], dtype=torch.int32, device="cuda")
+    k, v = (torch.randn((3, kv, dim), device="cuda").bfloat16() for _ in range(2))
+    inv = torch.zeros(0, device="cuda")
+    api.rm_rotary_append(None, k, v, inv, cache, table, lens, token_offsets=off, max_tokens=3)
+    gk, gv = api.rm_cache_read(cache, table.reshape(-1))
+    for got, x in ((gk, k), (gv, v)):
+        assert float((got[0, :3].float() - x.float()).abs().max()) <= float(x.abs().max()) / 120
+    q = torch.randn((1, kv, dim), device="cuda").bfloat16()
+    out = api.rm_cache_attention(q, cache, table, lens)
+    w = torch.softmax((gk[0, :3].double() * q.double()).sum(-1) / 16, dim=0)
+    want = (w[..., None] * gv[0, :3].double()).sum(0)
+    assert float((out[0].double() - want).abs().max()) < 0.02
+
+
+def test_values_that_are_not_finite_are_not_hidden():
+    for codes in (INT8, E4M3):
+        for bad in (float("nan"), float("inf")):
+            cache, table, lens, _ = make_cache([20, 20], 2, 16, 64, codes, 8)
+            k, v = (torch.randn((2, 2, 64), device="cuda").bfloat16() for _ in range(2))
+            v[0, 1, 5] = bad
+            api.rm_rotary_append(None, k, v, frequencies(64).cuda(), cache, table, lens)
+            q = torch.randn((2, 2, 64), device="cuda").bfloat16()
+            out = api.rm_cache_attention(q, cache, table, lens)
+            assert not torch.any(torch.isfinite(out[0, 1]))
+            assert torch.all(torch.isfinite(out[0, 0])) and torch.all(torch.isfinite(out[1]))
+
+
+def test_what_is_out_of_range_is_skipped_and_reported():
+    cache, table, lens, _ = make_cache([20, 20, 20], 1, 16, 64, INT8, 9)
+    k, v = (torch.randn((3, 1, 64), device="cuda").bfloat16() for _ in range(2))
+    inv = frequencies(64).cuda()
+    before = {n: t.clone() for n, t in cache.items()}
+    table[0, 1] = cache["k"].shape[0]
+    table[1, 1] = -1
+    lens[2] = 1000
+    st = api.new_status()
+    q = api.rm_rotary_append(k, k, v, inv, cache, table, lens, status=st)
+    assert int(st.item()) == api.ST_BAD_PAGE | api.ST_BAD_LENGTH
+    assert torch.all(torch.isfinite(q))
+    for n in cache:
+        assert torch.equal(cache[n].view(torch.uint8), before[n].view(torch.uint8)), n
+    # more tokens than max_tokens, and offsets behind the tokens
+    for off in ([0, 2, 3, 3], [0, 1, 2, 9], [2, 1, 2, 3]):
+        st.zero_()
+        lens.fill_(20)
+        api.rm_rotary_append(None, k, v, inv, cache, table, lens, status=st,
+                             token_offsets=torch.tensor(off, dtype=torch.int32, device="cuda"))
+        assert int(st.item()) & api.ST_BAD_LENGTH
+
+
+@pytest.mark.parametrize("codes", [INT8, E4M3], ids=["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("page,dim", [(16, 64), (32, 256), (128, 128)])
+def test_read(page, dim, dtype, codes):
+    cache, table, _, _ = make_cache([3 * page], 3, page, dim, codes, 10)
+    pages = torch.tensor([2, 0, 99, 1, -1], dtype=torch.int32, device="cuda")
+    st = api.new_status()
+    k, v = api.rm_cache_read(cache, pages, dtype, status=st)
+    assert int(st.item()) == api.ST_BAD_PAGE
+    for i, p in enumerate(pages.tolist()):
+        for got, name in ((k, "k"), (v, "v")):
+            if p in (0, 1, 2):
+                c = ref.codes_f64(cache[name][p]).float()
+                c = (c if name == "k" else c.transpose(1, 2)) * cache[name + "_scale"][p].cpu()[:, None, None]
+                assert torch.equal(got[i].cpu(), c.to(dtype).transpose(0, 1))
+            else:
+                assert torch.all(got[i] == 0)
+    assert api.rm_cache_read(cache, pages[:0], dtype)[0].shape[0] == 0
+
+
+def test_refusals():
+    cache, table, lens, _ = make_cache([20], 2, 16, 64, INT8, 11)
+    k = torch.randn((1, 2, 64), device="cuda").bfloat16()
+    inv = frequencies(64).cuda()
+
+    def call(**kw):
+        a = dict(q=k, k=k, v=k, inv_freq=inv, cache=cache, table=table, lengths=lens)
+        a.update(kw)
+        return api.rm_rotary_append(**a)
+    call()
+    small = api.new_cache(2, 2, 8, 64)
+    odd = api.new_cache(2, 2, 16, 96)
+    for kind, kw in [
+            (ValueError, dict(k=k.float())), (ValueError, dict(v=k.half())),
+            (ValueError, dict(q=k[:, :, :32])), (ValueError, dict(layout="pairs")),
+            (ValueError, dict(inv_freq=inv.double())), (ValueError, dict(lengths=lens.long())),
+            (ValueError, dict(table=table.reshape(-1))), (ValueError, dict(k=k.cpu())),
+            (ValueError, dict(cache=dict(cache, v=cache["k"]))),
+            (ValueError, dict(cache=dict(cache, k=cache["k"].float()))),
+            (ValueError, dict(positions=lens.long())),
+            (RuntimeError, dict(cache=small)), (RuntimeError, dict(max_tokens=0)),
+            (RuntimeError, dict(inv_freq=torch.zeros(33, device="cuda"))),
+            (RuntimeError, dict(cache=odd, k=torch.zeros((1, 2, 96), device="cuda").bfloat16(),
+                                v=torch.zeros((1, 2, 96), device="cuda").bfloat16(), q=None))]:
+        with pytest.raises(kind):
+            call(**kw)
+    with pytest.raises(ValueError):
+        api.rm_cache_read(cache, lens.long())
+    with pytest.raises(ValueError):
+        api.rm_cache_read(cache, lens, torch.float32)
+    with pytest.raises(ValueError):
+        api.new_cache(1, 1, 16, 64, torch.uint8)
