@@ -121,6 +121,7 @@ extern "C" {
 #define RM_MAX_OPT_CAPACITY      4  /* capacity of rm_place_optimal            */
 
 #define RM_MAX_NORM_WIDTH    32768  /* width of rm_norm_residual               */
+#define RM_MAX_W4_COLUMNS  2097152  /* k of rm_w4_linear                       */
 #define RM_MAX_SEQUENCES     65535  /* n_seqs of the cache calls               */
 
 /* Target-device descriptor: the SM limits of Eq. (1) and Eq. (2).
@@ -516,15 +517,20 @@ typedef struct {
  *   half.  scales [n][ceil(k/group)]; zeros uint8 [n][ceil(k/group)], values
  *   0..15 (NULL: 8 everywhere); bias [n] or NULL.  y: rows of n (SWIGLU: n/2)
  *   elements, y_stride apart.  Sums are fp32, each output is rounded once.
- *   An infinity in x gives NaN wherever its products meet.
+ *   An infinity in x may give NaN.
+ * Some sizes split the columns over workgroups and join the parts through the
+ *   workspace, rm_w4_linear_workspace_bytes bytes, 256-byte aligned (0 bytes:
+ *   none, workspace may be NULL).  The order of every sum is fixed.
  * Errors: RM_EINVAL (NULL pointer, rows < 0, n or k < 1, a stride below its
  *   row, group not a multiple of 32, SWIGLU with odd n, bad type or act),
- *   RM_EUNSUPPORTED (a k over 2^24), RM_ELAUNCH.
+ *   RM_EUNSUPPORTED (k > RM_MAX_W4_COLUMNS), RM_EWORKSPACE, RM_ELAUNCH.
  */
+size_t rm_w4_linear_workspace_bytes(int32_t rows, int32_t n, int32_t k, int32_t act);
 int rm_w4_linear(int32_t type, int32_t rows, int32_t n, int32_t k, const void* x,
                  int64_t x_stride, const uint8_t* codes, int64_t code_stride, int32_t group,
                  const void* scales, const uint8_t* zeros, const void* bias, int32_t act,
-                 void* y, int64_t y_stride, void* stream);
+                 void* y, int64_t y_stride, void* workspace, size_t workspace_bytes,
+                 void* stream);
 
 /*
  * rm_rotary_append -- turns the queries and keys of the call's tokens by their

@@ -120,8 +120,10 @@ def library():
         lib.rm_place_optimal.restype = ctypes.c_int
         f32, sz = ctypes.c_float, ctypes.c_size_t
         C, S = ctypes.POINTER(Cache), ctypes.POINTER(Sequences)
+        lib.rm_w4_linear_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        lib.rm_w4_linear_workspace_bytes.restype = sz
         lib.rm_w4_linear.argtypes = [i32, i32, i32, i32, P, i64, P, i64, i32, P, P, P, i32, P,
-                                     i64, P]
+                                     i64, P, sz, P]
         lib.rm_rotary_append.argtypes = [i32, C, S, i32, P, i64, i64, P, i64, i64, P, i64, i64, P,
                                          P, i32, i32, f32, P, P, P]
         lib.rm_cache_read.argtypes = [i32, C, i32, P, P, P, P, P]
@@ -497,7 +499,8 @@ def _sequences_of(table, lengths, token_offsets, n_tokens, max_tokens):
                      n, pages, n_tokens, max_tokens)
 
 
-def rm_w4_linear(x, codes, scales, group, zeros=None, bias=None, act="none", out=None):
+def rm_w4_linear(x, codes, scales, group, zeros=None, bias=None, act="none", out=None,
+                 workspace=None):
     """x [rows, k] through 4-bit weights: codes uint8 [n, ceil(k / 2)] (rows may
     be strided), even elements in the low half; scales [n, ceil(k / group)] of
     x's type; zeros uint8 like scales (None: 8); bias [n].  act "swiglu" takes
@@ -516,11 +519,18 @@ def rm_w4_linear(x, codes, scales, group, zeros=None, bias=None, act="none", out
     xp, xs = _rows(x, x.dtype, x.shape, "x")
     cp, cs = _rows(codes, torch.uint8, (n, (k + 1) // 2), "codes")
     op, os_ = _rows(out, x.dtype, (rows, n // 2 if act else n), "out")
-    code = library().rm_w4_linear(
+    lib = library()
+    if workspace is None:
+        need = lib.rm_w4_linear_workspace_bytes(rows, n, k, act)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    code = lib.rm_w4_linear(
         kind, rows, n, k, xp, _pitch(xs, rows, k, "x"), cp,
         _pitch(cs, n, (k + 1) // 2, "codes"), group,
         _on_gpu(scales, x.dtype, groups, "scales"), _on_gpu(zeros, torch.uint8, groups, "zeros"),
-        _on_gpu(bias, x.dtype, (n,), "bias"), act, op, _pitch(os_, rows, out.shape[1], "out"), _raw_stream(x))
+        _on_gpu(bias, x.dtype, (n,), "bias"), act, op, _pitch(os_, rows, out.shape[1], "out"),
+        workspace.data_ptr() if workspace is not None else None,
+        workspace.numel() if workspace is not None else 0, _raw_stream(x))
     if code:
         _check(code, "rm_w4_linear")
     return out

@@ -54,6 +54,15 @@ int check_seqs(const rm_sequences* s, const rm_cache* c)
     return RM_OK;
 }
 
+// floor(k / group) = umulhi(k / 32, inverse) for every column below k: the
+// product's error, k / 32 / 2^32, stays below 32 / group for k <= 2^21 (a group
+// beyond k counts as the next multiple of 32).
+uint32_t inverse_of(int32_t k, int32_t group)
+{
+    const uint32_t d = (uint32_t)(group < k ? group : k + 31) / 32;
+    return d <= 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + d - 1) / d);
+}
+
 }  // namespace
 
 void note_launch(const void* kernel, int64_t blocks, unsigned threads, size_t dynamic_lds)
@@ -76,10 +85,16 @@ void note_launch(const void* kernel, int64_t blocks, unsigned threads, size_t dy
 
 extern "C" {
 
+size_t rm_w4_linear_workspace_bytes(int32_t rows, int32_t n, int32_t k, int32_t act)
+{
+    if (rows < 1 || n < 1 || k < 1 || k > RM_MAX_W4_COLUMNS) return 0;
+    return rm::linear_workspace(rows, n, k, act);
+}
+
 int rm_w4_linear(int32_t type, int32_t rows, int32_t n, int32_t k, const void* x,
                  int64_t x_stride, const uint8_t* codes, int64_t code_stride, int32_t group,
                  const void* scales, const uint8_t* zeros, const void* bias, int32_t act,
-                 void* y, int64_t y_stride, void* stream)
+                 void* y, int64_t y_stride, void* workspace, size_t workspace_bytes, void* stream)
 {
     if (!rm::type_ok(type) || rows < 0 || n < 1 || k < 1 || group < 1 || group % 32)
         return RM_EINVAL;
@@ -87,10 +102,13 @@ int rm_w4_linear(int32_t type, int32_t rows, int32_t n, int32_t k, const void* x
     if (act == RM_ACT_SWIGLU && n % 2) return RM_EINVAL;
     const int32_t out = act == RM_ACT_SWIGLU ? n / 2 : n;
     if (x_stride < k || code_stride < (k + 1) / 2 || y_stride < out) return RM_EINVAL;
-    if (k > 1 << 24) return RM_EUNSUPPORTED;
+    if (k > RM_MAX_W4_COLUMNS) return RM_EUNSUPPORTED;
     if (rows == 0) return RM_OK;
     if (!x || !codes || !scales || !y) return RM_EINVAL;
-    rm::LinearArgs a = {rows, n, k, group, x, codes, scales, zeros, bias, y, x_stride,
+    const size_t need = rm::linear_workspace(rows, n, k, act);
+    if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255)))
+        return RM_EWORKSPACE;
+    rm::LinearArgs a = {rows, n, k, group, x, codes, scales, zeros, bias, y, workspace, rm::inverse_of(k, group), x_stride,
                         code_stride, y_stride};
     return rm::done(rm::launch_linear(type, act, a, (hipStream_t)stream));
 }

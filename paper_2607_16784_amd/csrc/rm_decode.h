@@ -163,9 +163,12 @@ struct LinearArgs {
     const void* scales;
     const uint8_t* zeros;
     const void* bias;
-    void* y;
+    void *y, *workspace;
+    uint32_t inverse;             // 2^32 / (group / 32), rounded up; 0 for 32
     int64_t x_stride, code_stride, y_stride;
 };
+// Workspace bytes of launch_linear; 0 where it needs none.
+size_t linear_workspace(int32_t rows, int32_t n, int32_t k, int act);
 hipError_t launch_linear(int type, int act, const LinearArgs& a, hipStream_t s);
 
 struct AppendArgs {

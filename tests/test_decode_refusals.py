@@ -31,15 +31,23 @@ def seqs(**kw):
 
 def test_w4_linear(lib):
     def call(type=0, rows=1, n=8, k=64, x=P, xs=64, codes=P, cs=32, group=32, scales=P, act=0,
-             y=P, ys=8):
+             y=P, ys=8, ws=None, size=0):
         return lib.rm_w4_linear(type, rows, n, k, x, xs, codes, cs, group, scales, None, None,
-                                act, y, ys, None)
+                                act, y, ys, ws, size, None)
     assert call(rows=0) == 0
     for kw in (dict(type=2), dict(rows=-1), dict(n=0), dict(k=0), dict(xs=63), dict(cs=31),
                dict(group=0), dict(group=40), dict(act=2), dict(act=1, n=7, ys=7), dict(ys=7),
                dict(x=None), dict(codes=None), dict(scales=None), dict(y=None)):
         assert call(**kw) == 1, kw
     assert call(k=1 << 25, xs=1 << 25, cs=1 << 24) == 3
+    # sizes whose columns are split need a workspace
+    big = dict(rows=64, n=512, k=8192, xs=8192, cs=4096, ys=512)
+    need = lib.rm_w4_linear_workspace_bytes(64, 512, 8192, 0)
+    assert need > 0 and need % 4 == 0
+    assert lib.rm_w4_linear_workspace_bytes(1, 512, 8192, 0) == 0
+    assert lib.rm_w4_linear_workspace_bytes(0, 512, 8192, 0) == 0
+    for kw in (dict(), dict(ws=P, size=need - 1), dict(ws=ctypes.c_void_p(257), size=need)):
+        assert call(**big, **kw) == 2, kw
 
 
 BAD_CACHES = [(dict(k=None), 1), (dict(v=None), 1), (dict(k_scale=None), 1), (dict(n_pages=0), 1),

@@ -57,6 +57,18 @@ CASES = [
     (130, 20, 200, 224, True, False, "swiglu"),
     (5, 2, 2048, 1024, True, True, "swiglu"),
     (1, 200, 9001, 128, True, False, "none"),
+    # every form: whole in LDS, wide, streams of one, two and four tiles, split
+    (2, 16500, 300, 32, True, False, "none"),
+    (3, 33000, 260, 128, False, True, "swiglu"),
+    (16, 8300, 1056, 64, True, False, "none"),
+    (9, 16600, 320, 32, False, False, "swiglu"),
+    (16, 96, 11000, 128, False, False, "none"),
+    (16, 64, 24000, 32, True, False, "none"),
+    (20, 500, 9000, 96, True, True, "none"),
+    (32, 130, 5000, 256, True, False, "swiglu"),
+    (64, 300, 4100, 32, True, True, "none"),
+    (61, 260, 9216, 128, True, False, "swiglu"),
+    (200, 270, 2600, 64, False, True, "none"),
 ]
 
 
