@@ -1,7 +1,7 @@
 // attend.hip -- attention over the paged 8-bit cache (rm_cache_attention).
 //
 // The rows of a tile are the (token, query head) pairs that share a kv head,
-// tokens first: 16 for a decode step, up to 64 for a chunk of a prompt.  A wave
+// tokens first: 16 for a decode step, 32 for a chunk of a prompt.  A wave
 // takes 64 cached tokens at a time, all in registers, with the running maximum
 // and sum of the softmax:
 //   S^T = K Q^T   v_mfma_f32_16x16x32 in q's type, keys as the 16 rows
@@ -26,6 +26,7 @@ namespace {
 
 constexpr int kBlock = 64;    // cached tokens a wave takes at a time
 constexpr int kWaves = 4;
+constexpr int kMostSplits = 256;
 
 __device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c)
 {
@@ -83,6 +84,7 @@ __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 struct Plan {
     int32_t tiles, splits;      // tiles of rows a sequence and kv head; splits of a tile
+    int32_t rows;               // of a tile that a sequence can have
 };
 
 // Rows and token range of a tile.
@@ -105,14 +107,17 @@ __device__ inline Tile tile_of(const Sequence& s, int32_t group, int32_t window,
     return t;
 }
 
+// Two waves a SIMD where the registers allow it: left to itself the compiler
+// takes all registers for one (32 rows, chunks of prompts: 209 us, with two 134).
 template <typename T, int FMT, int D, int C>
-__global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a, Plan plan)
+__global__ __launch_bounds__(kWaves * 64)
+__attribute__((amdgpu_waves_per_eu(D <= 128 ? 2 : 1))) void
+attend_kernel(AttendArgs a, Plan plan)
 {
     typedef typename Vec<T>::x8 V;
-    constexpr int H = 16 * C;                  // rows of a tile
-    constexpr int PITCH = D + 4;
-    __shared__ float join[H * PITCH];
-    __shared__ float join_m[kWaves][H], join_l[kWaves][H], join_s[kWaves];
+    constexpr int H = 16 * C, W = kWaves;      // rows of a tile
+    extern __shared__ __align__(16) float join[];
+    __shared__ float join_m[W][H], join_l[W][H];
 
     const int KV = a.cache.kv_heads, TK = a.cache.page_tokens, G = a.heads / KV;
     int64_t at = blockIdx.x;
@@ -122,7 +127,8 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a, Plan 
     at /= plan.tiles;
     const int head = (int)(at % KV), b = (int)(at / KV);
     const Sequence s = sequence_of(a.seqs, TK, b);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, quad = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int li = lane & 15, quad = lane >> 4;
 
     if (s.n == 0) {
         // no token, or one of a sequence that is out of range: zeros
@@ -132,7 +138,7 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a, Plan 
         if (a.seqs.token_offsets) from = s.first, upto = a.seqs.token_offsets[b + 1];
         if (from < 0 || upto > a.seqs.n_tokens) return;
         for (int64_t t = from; t < upto; ++t)
-            for (int i = threadIdx.x; i < G * D; i += kWaves * 64)
+            for (int i = threadIdx.x; i < G * D; i += W * 64)
                 static_cast<T*>(a.out)[(t * a.heads + head * G) * D + i] = (T)0.0f;
         return;
     }
@@ -142,10 +148,64 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a, Plan 
     const int per = (b1 - b0 + plan.splits - 1) / plan.splits;
     const int from = b0 + split * per, upto = min(b1, from + per);
 
+    const int32_t* table = a.seqs.table + (int64_t)b * a.seqs.table_stride;
+    const int shift = __ffs(TK) - 1, last_page = (s.length - 1) >> shift;
+    // the pages of the 16 tokens of a block whose keys and whose values the lane
+    // loads; an id out of range becomes page 0 and the tokens are not seen
+    struct Pages {
+        int32_t k, v;
+        bool bad;
+    };
+    auto ids = [&](int block) {
+        const int t0 = block * kBlock;
+        Pages p;
+        p.k = table[min((t0 + (li >> 2) * 16) >> shift, last_page)];
+        p.v = table[min((t0 + quad * 16) >> shift, last_page)];
+        return p;
+    };
+    auto checked = [&](Pages p) {
+        p.bad = (uint32_t)p.v >= (uint32_t)a.cache.n_pages;
+        if (p.bad) p.v = 0;
+        if ((uint32_t)p.k >= (uint32_t)a.cache.n_pages) p.k = 0;
+        return p;
+    };
+    u32x4 kc[4][D / 64], vc[D / 16];
+    float ks, vs;
+    auto load_k = [&](int block, const Pages& p) {
+        const int tk = block * kBlock + (li >> 2) * 16;
+        const uint8_t* kp = static_cast<const uint8_t*>(a.cache.k) +
+                            (((int64_t)p.k * KV + head) * TK + (tk & (TK - 1)) + (li & 3)) * D +
+                            quad * 16;
+        ks = a.cache.k_scale[(int64_t)p.v * KV + head];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j)
+                kc[i][j] = *reinterpret_cast<const u32x4*>(kp + i * 4 * D + j * 64);
+    };
+    auto load_v = [&](int block, const Pages& p) {
+        const int tv = block * kBlock + quad * 16;
+        const int64_t bv = (int64_t)p.v * KV + head;
+        const uint8_t* vp = static_cast<const uint8_t*>(a.cache.v) + (bv * D + li) * TK +
+                            (tv & (TK - 1));
+        vs = a.cache.v_scale[bv];
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d)
+            vc[d] = *reinterpret_cast<const u32x4*>(vp + d * 16 * TK);
+    };
+
     // queries: row 16 c + li of the tile, channels 64 j + 16 quad + 8 k of the
     // operand for the k-th half of the j-th 16-byte load of keys
     V q[C][D / 32];
     int32_t pos[C];
+    f32x4 o[D / 16][C];
+    float m[C], l[C], ref = 0.0f;              // ref: largest scale of values so far
+    Pages now, next;
+    int block = from + wave;
+    if (block < upto) {
+        now = ids(block);
+        next = ids(min(block + W, upto - 1));
+    }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int r = tile * H + min(c * 16 + li, t.rows - 1);
@@ -156,9 +216,6 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a, Plan 
         for (int k = 0; k < D / 32; ++k)
             q[c][k] = load8(row + (k >> 1) * 64 + quad * 16 + (k & 1) * 8);
     }
-
-    f32x4 o[D / 16][C];
-    float m[C], l[C], ref = 0.0f;              // ref: largest scale of values so far
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         m[c] = -INFINITY;
@@ -166,35 +223,16 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a, Plan 
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) o[d][c] = f32x4{0, 0, 0, 0};
     }
-    const int32_t* table = a.seqs.table + (int64_t)b * a.seqs.table_stride;
-    const int shift = __ffs(TK) - 1, last_page = (s.length - 1) >> shift;
     const float to_log2 = a.scale * 1.44269504088896340736f;
     int32_t st = 0;
-
-    for (int block = from + wave; block < upto; block += kWaves) {
-        const int t0 = block * kBlock;
-        // the pages of the 16 tokens whose keys and whose values the lane loads
-        const int tk = t0 + (li >> 2) * 16, tv = t0 + quad * 16;
-        int32_t pk = table[min(tk >> shift, last_page)], pv = table[min(tv >> shift, last_page)];
-        const bool bad = pv < 0 || pv >= a.cache.n_pages;
-        if (bad) st = RM_ST_BAD_PAGE, pv = 0;
-        if (pk < 0 || pk >= a.cache.n_pages) pk = 0;
-        const int64_t bk = (int64_t)pk * KV + head, bv = (int64_t)pv * KV + head;
-        const uint8_t* kp = static_cast<const uint8_t*>(a.cache.k) +
-                            (bk * TK + (tk & (TK - 1)) + (li & 3)) * D + quad * 16;
-        const uint8_t* vp = static_cast<const uint8_t*>(a.cache.v) + (bv * D + li) * TK + (tv & (TK - 1));
-        u32x4 kc[4][D / 64], vc[D / 16];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < D / 64; ++j)
-                kc[i][j] = *reinterpret_cast<const u32x4*>(kp + i * 4 * D + j * 64);
-        const float ks = a.cache.k_scale[bv] * to_log2;
-        const float vs = a.cache.v_scale[bv];
-#pragma unroll
-        for (int d = 0; d < D / 16; ++d)
-            vc[d] = *reinterpret_cast<const u32x4*>(vp + d * 16 * TK);
-
+    if (block < upto) {
+        now = checked(now);
+        load_k(block, now);
+        load_v(block, now);
+    }
+    for (; block < upto; block += W) {
+        const int t0 = block * kBlock, tv = t0 + quad * 16;
+        const int following = min(block + W, upto - 1);      // the last block again at the end
         f32x4 sc[4][C];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -208,6 +246,16 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a, Plan 
                 for (int c = 0; c < C; ++c) sc[i][c] = mfma(e, q[c][k], sc[i][c]);
             }
         }
+        // the next block's keys fly while this one's weights are taken, its values
+        // while its keys are multiplied, and the page after it is looked up
+        __builtin_amdgcn_sched_barrier(0);         // the codes stay codes until their turn
+        const float k_log2 = ks * to_log2;
+        const bool bad = now.bad;
+        if (bad) st = RM_ST_BAD_PAGE;
+        next = checked(next);
+        load_k(following, next);
+        const Pages after = ids(min(following + W, upto - 1));
+        __builtin_amdgcn_sched_barrier(0);
         const bool whole = t0 >= t.all_lo && t0 + kBlock <= t.all_hi && !__any(bad);
         float top[C];
         bool moved = false;
@@ -218,7 +266,7 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a, Plan 
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    float v = sc[i][c][k] * ks;
+                    float v = sc[i][c][k] * k_log2;
                     if (!whole) {
                         const int token = tv + 4 * i + k;
                         const bool seen = token <= pos[c] && !bad &&
@@ -231,9 +279,10 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a, Plan 
             top[c] = fmaxf(m[c], rows_reduce<Max>(x));
             moved |= top[c] > m[c];
         }
-        const float now = fmaxf(ref, rows_reduce<Max>(bad ? 0.0f : vs));
-        if (__any(moved || now > ref)) {
-            const float shrink = now > 0.0f ? ref / now : 1.0f;
+        const float v_scale = vs;
+        const float largest = fmaxf(ref, rows_reduce<Max>(bad ? 0.0f : v_scale));
+        if (__any(moved || largest > ref)) {
+            const float shrink = largest > 0.0f ? ref / largest : 1.0f;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const float f = top[c] == -INFINITY ? 1.0f : exp2_of(m[c] - top[c]);
@@ -242,9 +291,9 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a, Plan 
 #pragma unroll
                 for (int d = 0; d < D / 16; ++d) o[d][c] *= f * shrink;
             }
-            ref = now;
+            ref = largest;
         }
-        const float share = ref > 0.0f ? vs / ref : 0.0f;
+        const float share = ref > 0.0f ? v_scale / ref : 0.0f;
         f16x8 p[2][C];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
@@ -279,59 +328,79 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a, Plan 
 #pragma unroll
                 for (int c = 0; c < C; ++c) o[d][c] = mfma(e, p[k][c], o[d][c]);
             }
+        __builtin_amdgcn_sched_barrier(0);
+        load_v(following, next);
+        __builtin_amdgcn_sched_barrier(0);
+        now = next;
+        next = after;
     }
     report_status(a.status, st);
 
-    // join the waves: common maximum, then the sums one wave after the other
+    // join the waves: common maximum, then the upper half's sums onto the lower
+    // half's, and so on
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         l[c] = rows_reduce<Add>(l[c]);
         if (quad == 0) join_m[wave][c * 16 + li] = m[c], join_l[wave][c * 16 + li] = l[c];
     }
     __syncthreads();
-    float f[C];
+    // [wave][d / 4][row][4]: neighbouring lanes write neighbouring rows
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         float top = join_m[0][c * 16 + li];
-        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, join_m[w][c * 16 + li]);
-        f[c] = exp2_of(m[c] - (top == -INFINITY ? 0.0f : top)) * ref;
+        for (int w = 1; w < W; ++w) top = fmaxf(top, join_m[w][c * 16 + li]);
+        const float f = exp2_of(m[c] - (top == -INFINITY ? 0.0f : top)) * ref;
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) o[d][c] *= f;
     }
-    for (int w = 0; w < kWaves; ++w) {
-        if (wave == w) {
+    f32x4* sums = reinterpret_cast<f32x4*>(join);
+    auto place = [&](int w, int d, int c) { return ((w * (D / 4) + d * 4 + quad) * H) + c * 16 + li; };
+#pragma unroll
+    for (int half = W / 2; half > 0; half >>= 1) {
+        if (wave >= half && wave < 2 * half) {
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int d = 0; d < D / 16; ++d) {
-                    f32x4* to = reinterpret_cast<f32x4*>(
-                        &join[(c * 16 + li) * PITCH + d * 16 + quad * 4]);
-                    const f32x4 mine = o[d][c] * f[c];
-                    *to = w == 0 ? mine : *to + mine;
-                }
+                for (int d = 0; d < D / 16; ++d) sums[place(wave - half, d, c)] = o[d][c];
+        }
+        __syncthreads();
+        if (wave < half) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int d = 0; d < D / 16; ++d) o[d][c] += sums[place(wave, d, c)];
         }
         __syncthreads();
     }
+    if (wave == 0) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) sums[place(0, d, c)] = o[d][c];
+    }
+    __syncthreads();
     float* part = static_cast<float*>(a.workspace);
     const int64_t n_parts = (int64_t)gridDim.x;
-    for (int u = threadIdx.x; u < t.rows * (D / 8); u += kWaves * 64) {
+    for (int u = threadIdx.x; u < t.rows * (D / 8); u += W * 64) {
         const int row = u / (D / 8), d = u % (D / 8) * 8;
         float top = join_m[0][row];
-        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, join_m[w][row]);
+        for (int w = 1; w < W; ++w) top = fmaxf(top, join_m[w][row]);
         const float base = top == -INFINITY ? 0.0f : top;
         float sum = 0.0f;
-        for (int w = 0; w < kWaves; ++w) sum += join_l[w][row] * exp2_of(join_m[w][row] - base);
-        const float* from_row = &join[row * PITCH + d];
+        for (int w = 0; w < W; ++w) sum += join_l[w][row] * exp2_of(join_m[w][row] - base);
+        const f32x4 v0 = sums[(d / 4) * H + row], v1 = sums[(d / 4 + 1) * H + row];
         if (plan.splits == 1) {
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
             V r;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) r[i] = (T)(from_row[i] * inv);
+            for (int i = 0; i < 4; ++i) r[i] = (T)(v0[i] * inv), r[4 + i] = (T)(v1[i] * inv);
             const int rr = tile * H + row;
             store8(static_cast<T*>(a.out) +
                        ((int64_t)(s.first + rr / G) * a.heads + head * G + rr % G) * D + d, r);
         } else {
             float* to = part + ((int64_t)blockIdx.x * H + row) * D + d;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) to[i] = from_row[i];
+            reinterpret_cast<f32x4*>(to)[0] = v0;
+            reinterpret_cast<f32x4*>(to)[1] = v1;
             if (d == 0) {
                 float* ml = part + n_parts * H * D + ((int64_t)blockIdx.x * H + row) * 2;
                 ml[0] = top;
@@ -341,68 +410,90 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(AttendArgs a, Plan 
     }
 }
 
-// One wave a row of a tile: the splits' partial results, in order.
+// A workgroup a row of a tile: the splits' partial results.  A wave takes every
+// fourth split, a lane the splits' maxima and sums first.
 template <typename T, int D, int C>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, Plan plan, int64_t n_parts)
 {
-    constexpr int H = 16 * C;
+    constexpr int H = 16 * C, N = D / 64;
+    __shared__ float factor[kMostSplits];
+    __shared__ float sums[4][D];
     const int KV = a.cache.kv_heads, G = a.heads / KV;
-    const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 6;
-    const int lane = threadIdx.x & 63;
-    int64_t at = unit;
-    const int row = (int)(at % H);
-    at /= H;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t at = blockIdx.x;
+    const int row = (int)(at % plan.rows);
+    at /= plan.rows;
     const int64_t block = at * plan.splits;
     const int tile = (int)(at % plan.tiles);
     at /= plan.tiles;
     const int head = (int)(at % KV);
-    if (at / KV >= a.seqs.n_seqs) return;
     const Sequence s = sequence_of(a.seqs, a.cache.page_tokens, (int)(at / KV));
     const int rr = tile * H + row;
     if (rr >= s.n * G) return;
     const float* part = static_cast<const float*>(a.workspace);
     const float* ml = part + n_parts * H * D + (block * H + row) * 2;
+    // every wave the same: one split a lane, then the next 64
     float top = -INFINITY;
-    for (int i = 0; i < plan.splits; ++i) top = fmaxf(top, ml[(int64_t)i * H * 2]);
+    for (int i = lane; i < plan.splits; i += 64) top = fmaxf(top, ml[(int64_t)i * H * 2]);
+    top = wave_reduce<Max>(top);
     const float base = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, v[D / 64];
-#pragma unroll
-    for (int k = 0; k < D / 64; ++k) v[k] = 0.0f;
-    for (int i = 0; i < plan.splits; ++i) {
-        const float li = ml[(int64_t)i * H * 2 + 1];
-        if (li == 0.0f) continue;                   // saw nothing
-        const float f = exp2_of(ml[(int64_t)i * H * 2] - base);
-        sum = __builtin_fmaf(li, f, sum);
-        const float* from = part + ((block + i) * H + row) * D;
-#pragma unroll
-        for (int k = 0; k < D / 64; ++k) v[k] = __builtin_fmaf(from[k * 64 + lane], f, v[k]);
+    float sum = 0.0f;
+    for (int i = lane; i < plan.splits; i += 64) {
+        const float f = exp2_of(ml[(int64_t)i * H * 2] - base), l = ml[(int64_t)i * H * 2 + 1];
+        sum = __builtin_fmaf(l, f, sum);
+        // a split that saw nothing may not have written its sums
+        if (wave == 0) factor[i] = l == 0.0f ? -1.0f : f;
     }
+    sum = wave_reduce<Add>(sum);
+    __syncthreads();
+    float v[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = 0.0f;
+    const float* from = part + (block * H + row) * D + lane * N;
+    typedef float Vn __attribute__((ext_vector_type(N)));
+#pragma unroll 4
+    for (int i = wave; i < plan.splits; i += 4) {
+        const float f = factor[i];
+        const Vn x = *reinterpret_cast<const Vn*>(from + (int64_t)i * H * D);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            v[k] = f < 0.0f ? v[k] : __builtin_fmaf(x[k], f, v[k]);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) sums[wave][lane * N + k] = v[k];
+    __syncthreads();
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     T* out = static_cast<T*>(a.out) +
              ((int64_t)(s.first + rr / G) * a.heads + head * G + rr % G) * D;
-#pragma unroll
-    for (int k = 0; k < D / 64; ++k) out[k * 64 + lane] = (T)(v[k] * inv);
+    for (int d = threadIdx.x; d < D; d += 256)
+        out[d] = (T)((sums[0][d] + sums[1][d] + sums[2][d] + sums[3][d]) * inv);
 }
 
-int columns_of(int32_t head_dim, int64_t rows)
+// 64 rows a tile need all registers of a SIMD for one wave: chunks of prompts
+// took 238 us with 64, 134 with 32, 182 with 16.
+int columns_of(int64_t rows)
 {
-    if (rows <= 16) return 1;
-    if (rows <= 32 || head_dim > 128) return 2;
-    return 4;
+    return rows <= 16 ? 1 : 2;
 }
 
 Plan plan_of(const rm_cache& c, const rm_sequences& s, int32_t heads)
 {
     const int64_t rows = (int64_t)s.max_tokens * (heads / c.kv_heads);
-    const int height = 16 * columns_of(c.head_dim, rows);
+    const int height = 16 * columns_of(rows);
     Plan p;
     p.tiles = (int32_t)((rows + height - 1) / height);
+    p.rows = (int32_t)(rows < height ? rows : height);
     const int64_t units = (int64_t)s.n_seqs * c.kv_heads * p.tiles;
-    // two workgroups a CU where the tokens reach: a wave has one block at least
+    // Two workgroups a CU, as far as every wave has two blocks of the longest
+    // possible sequence.  One sequence of 501 tokens: 10.9 us in one part, 11.6 in
+    // two; two of 125 000: 108 us in 32 parts, 115 in 64; 64 ragged ones of up to
+    // 4096, 512 workgroups already: 68 us, in two parts 84.
     const int64_t blocks = ((int64_t)s.table_stride * c.page_tokens + kBlock - 1) / kBlock;
-    const int64_t want = units > 0 ? (2 * kComputeUnits + units - 1) / units : 1;
-    const int64_t most = (blocks + kWaves - 1) / kWaves;
+    const int64_t want = units > 0 ? 2 * kComputeUnits / units : 1;
+    const int64_t most = blocks / (2 * kWaves);
     p.splits = (int32_t)(want < most ? want : most);
+    if (p.splits > kMostSplits) p.splits = kMostSplits;
     if (p.splits < 1) p.splits = 1;
     return p;
 }
@@ -413,23 +504,28 @@ hipError_t launch_columns(const AttendArgs& a, const Plan& p, hipStream_t s)
     const int64_t units = (int64_t)a.seqs.n_seqs * a.cache.kv_heads * p.tiles;
     const int64_t parts = units * p.splits;
     if (parts == 0) return hipSuccess;
-    if (parts > 0x7fffffff) return hipErrorInvalidValue;
-    hipError_t e = launch(attend_kernel<T, FMT, D, C>, dim3((unsigned)parts), kWaves * 64, 0, s,
-                          a, p);
+    if (parts > 0x7fffffff || units * p.rows > 0x7fffffff) return hipErrorInvalidValue;
+    const size_t lds = (size_t)(kWaves / 2) * 16 * C * D * sizeof(float);    // 64 KB at most
+    const auto kernel = attend_kernel<T, FMT, D, C>;
+    if (lds > 60 * 1024) {      // with the static arrays over 64 KB
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    hipError_t e = launch(kernel, dim3((unsigned)parts), kWaves * 64, lds, s, a, p);
     if (e != hipSuccess || p.splits == 1) return e;
-    return launch(attend_join_kernel<T, D, C>, dim3((unsigned)(units * 16 * C / 4)), 256, 0, s, a,
-                  p, parts);
+    return launch(attend_join_kernel<T, D, C>, dim3((unsigned)(units * p.rows)), 256, 0, s, a, p,
+                  parts);
 }
 
 template <typename T, int FMT, int D>
 hipError_t launch_dim(const AttendArgs& a, hipStream_t s)
 {
     const Plan p = plan_of(a.cache, a.seqs, a.heads);
-    const int c = columns_of(D, (int64_t)a.seqs.max_tokens * (a.heads / a.cache.kv_heads));
-    if (c == 1) return launch_columns<T, FMT, D, 1>(a, p, s);
-    if (c == 2) return launch_columns<T, FMT, D, 2>(a, p, s);
-    if constexpr (D <= 128) return launch_columns<T, FMT, D, 4>(a, p, s);
-    return hipErrorInvalidValue;
+    if (columns_of((int64_t)a.seqs.max_tokens * (a.heads / a.cache.kv_heads)) == 1)
+        return launch_columns<T, FMT, D, 1>(a, p, s);
+    return launch_columns<T, FMT, D, 2>(a, p, s);
 }
 
 template <typename T, int FMT>
@@ -446,7 +542,7 @@ size_t attend_workspace(const rm_cache& c, const rm_sequences& s, int32_t heads)
 {
     const Plan p = plan_of(c, s, heads);
     if (p.splits == 1) return 256;
-    const int height = 16 * columns_of(c.head_dim, (int64_t)s.max_tokens * (heads / c.kv_heads));
+    const int height = 16 * columns_of((int64_t)s.max_tokens * (heads / c.kv_heads));
     const size_t parts = (size_t)s.n_seqs * c.kv_heads * p.tiles * p.splits;
     return (parts * height * (c.head_dim + 2) * sizeof(float) + 255) / 256 * 256;
 }
