@@ -413,25 +413,28 @@ def rm_place_optimal(delay, iso_time, kernel_count, models, n_devices, capacity,
 
 # ---- kernels of a decode layer ---------------------------------------------
 
+# These run before every launch of a few microseconds, so they are written for
+# the accepted case: one expression, the message only where it fails.
+
 def _on_gpu(t, dtype, shape, name):
     """Address of a contiguous GPU tensor of this type and shape; None for None."""
     if t is None:
         return None
-    if not t.is_cuda or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous GPU tensor of {dtype} and shape "
-                         f"{tuple(shape)}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
+    if t.is_cuda and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name}: expected a contiguous GPU tensor of {dtype} and shape "
+                     f"{tuple(shape)}, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 def _rows(t, dtype, shape, name):
-    """Address and leading strides of a GPU tensor whose last axis is consecutive."""
-    if not t.is_cuda or t.dtype != dtype or t.shape != shape:
-        raise ValueError(f"{name}: expected a GPU tensor of {dtype} and shape {tuple(shape)}, "
-                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-    strides = t.stride()
-    if strides[-1] != 1 and shape[-1] > 1:
+    """Strides of a GPU tensor whose last axis is consecutive."""
+    if t.is_cuda and t.dtype is dtype and t.shape == shape:
+        strides = t.stride()
+        if strides[-1] == 1 or shape[-1] <= 1:
+            return strides
         raise ValueError(f"{name}: the last axis must be consecutive")
-    return (t.data_ptr(),) + strides[:-1]
+    raise ValueError(f"{name}: expected a GPU tensor of {dtype} and shape {tuple(shape)}, "
+                     f"got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 def _pitch(stride, rows, width, name):
@@ -458,8 +461,7 @@ def _named(names, value, what):
     return code
 
 
-def _raw_stream(t):
-    return torch._C._cuda_getCurrentRawStream(t.device.index)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def new_cache(n_pages, kv_heads, page_tokens, head_dim, codes=torch.int8, device="cuda"):
@@ -477,23 +479,24 @@ def new_cache(n_pages, kv_heads, page_tokens, head_dim, codes=torch.int8, device
 
 
 def _cache_of(cache):
-    k = cache["k"]
-    if k.dim() != 4 or k.dtype not in CODES:
+    k, v, ks, vs = cache["k"], cache["v"], cache["k_scale"], cache["v_scale"]
+    codes = CODES.get(k.dtype)
+    if k.dim() != 4 or codes is None:
         raise ValueError("cache: expected codes int8 or float8_e4m3fn [pages, kv_heads, "
                          f"page_tokens, head_dim], got {k.dtype} {tuple(k.shape)}")
-    pages, heads, tokens, dim = k.shape
-    return Cache(_on_gpu(k, k.dtype, k.shape, "cache k"),
-                 _on_gpu(cache["v"], k.dtype, (pages, heads, dim, tokens), "cache v"),
-                 _on_gpu(cache["k_scale"], torch.float32, (pages, heads), "cache k_scale"),
-                 _on_gpu(cache["v_scale"], torch.float32, (pages, heads), "cache v_scale"),
-                 pages, heads, tokens, dim, CODES[k.dtype])
+    shape = pages, heads, tokens, dim = k.shape
+    return Cache(_on_gpu(k, k.dtype, shape, "cache k"),
+                 _on_gpu(v, k.dtype, (pages, heads, dim, tokens), "cache v"),
+                 _on_gpu(ks, torch.float32, (pages, heads), "cache k_scale"),
+                 _on_gpu(vs, torch.float32, (pages, heads), "cache v_scale"),
+                 pages, heads, tokens, dim, codes)
 
 
 def _sequences_of(table, lengths, token_offsets, n_tokens, max_tokens):
     if table.dim() != 2:
         raise ValueError("table: expected [sequences, pages]")
-    n, pages = table.shape
-    return Sequences(_on_gpu(table, torch.int32, (n, pages), "table"),
+    n, pages = shape = table.shape
+    return Sequences(_on_gpu(table, torch.int32, shape, "table"),
                      _on_gpu(lengths, torch.int32, (n,), "lengths"),
                      _on_gpu(token_offsets, torch.int32, (n + 1,), "token_offsets"),
                      n, pages, n_tokens, max_tokens)
@@ -505,32 +508,37 @@ def rm_w4_linear(x, codes, scales, group, zeros=None, bias=None, act="none", out
     be strided), even elements in the low half; scales [n, ceil(k / group)] of
     x's type; zeros uint8 like scales (None: 8); bias [n].  act "swiglu" takes
     the first half of the outputs as gates of the second."""
-    kind = _type_of(x, "x")
+    kind, dtype = _type_of(x, "x"), x.dtype
     if x.dim() != 2 or codes.dim() != 2:
         raise ValueError("rm_w4_linear: expected x [rows, k] and codes [n, ceil(k / 2)]")
-    rows, k = x.shape
+    rows, k = shape = x.shape
     n = codes.shape[0]
     if group < 1 or group % 32:
         raise ValueError(f"group: expected a multiple of 32, got {group}")
+    row_bytes = (k + 1) // 2
     groups = (n, -(-k // group))
     act = _named(ACT_NAMES, act, "act")
+    width = n // 2 if act else n
     if out is None:
-        out = torch.empty((rows, n // 2 if act else n), dtype=x.dtype, device=x.device)
-    xp, xs = _rows(x, x.dtype, x.shape, "x")
-    cp, cs = _rows(codes, torch.uint8, (n, (k + 1) // 2), "codes")
-    op, os_ = _rows(out, x.dtype, (rows, n // 2 if act else n), "out")
-    lib = library()
+        out = x.new_empty((rows, width))
+        out_pitch = width
+    else:
+        out_pitch = _pitch(_rows(out, dtype, (rows, width), "out")[0], rows, width, "out")
+    x_pitch = _pitch(_rows(x, dtype, shape, "x")[0], rows, k, "x")
+    code_pitch = _pitch(_rows(codes, torch.uint8, (n, row_bytes), "codes")[0], n, row_bytes,
+                        "codes")
+    args = (kind, rows, n, k, x.data_ptr(), x_pitch, codes.data_ptr(), code_pitch, group,
+            _on_gpu(scales, dtype, groups, "scales"),
+            _on_gpu(zeros, torch.uint8, groups, "zeros"),
+            _on_gpu(bias, dtype, (n,), "bias"), act, out.data_ptr(), out_pitch)
+    lib, stream = _lib or library(), _raw_stream(x.get_device())
     if workspace is None:
-        need = lib.rm_w4_linear_workspace_bytes(rows, n, k, act)
-        if need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
-    code = lib.rm_w4_linear(
-        kind, rows, n, k, xp, _pitch(xs, rows, k, "x"), cp,
-        _pitch(cs, n, (k + 1) // 2, "codes"), group,
-        _on_gpu(scales, x.dtype, groups, "scales"), _on_gpu(zeros, torch.uint8, groups, "zeros"),
-        _on_gpu(bias, x.dtype, (n,), "bias"), act, op, _pitch(os_, rows, out.shape[1], "out"),
-        workspace.data_ptr() if workspace is not None else None,
-        workspace.numel() if workspace is not None else 0, _raw_stream(x))
+        code = lib.rm_w4_linear(*args, None, 0, stream)
+        if code == RM_EWORKSPACE:     # most sizes need none, so it is asked for only then
+            workspace = torch.empty(lib.rm_w4_linear_workspace_bytes(rows, n, k, act),
+                                    dtype=torch.uint8, device=x.device)
+    if workspace is not None:
+        code = lib.rm_w4_linear(*args, workspace.data_ptr(), workspace.numel(), stream)
     if code:
         _check(code, "rm_w4_linear")
     return out
@@ -543,30 +551,33 @@ def rm_rotary_append(q, k, v, inv_freq, cache, table, lengths, token_offsets=Non
     appends k and v to the cache, whose `lengths` count the call's tokens
     already.  q, k and v may be views of one projection.  Returns the turned
     q (None for q None)."""
-    kind = _type_of(k, "k")
+    kind, dtype = _type_of(k, "k"), k.dtype
     c = _cache_of(cache)
     if k.dim() != 3:
         raise ValueError("k: expected [tokens, kv_heads, head_dim]")
     tokens, dim = k.shape[0], c.head_dim
+    shape = (tokens, c.kv_heads, dim)
     s = _sequences_of(table, lengths, token_offsets, tokens, max_tokens)
-    kp, ks, kh = _rows(k, k.dtype, (tokens, c.kv_heads, dim), "k")
-    vp, vs, vh = _rows(v, k.dtype, (tokens, c.kv_heads, dim), "v")
-    heads, qp, qs, qh = 0, None, 0, 0
+    ks, vs = _rows(k, dtype, shape, "k"), _rows(v, dtype, shape, "v")
+    heads, qp, qs, op = 0, None, (0, 0), None
     if q is not None:
         if q.dim() != 3:
             raise ValueError("q: expected [tokens, heads, head_dim]")
         heads = q.shape[1]
-        qp, qs, qh = _rows(q, k.dtype, (tokens, heads, dim), "q")
+        shape = (tokens, heads, dim)
+        qs, qp = _rows(q, dtype, shape, "q"), q.data_ptr()
         if q_out is None:
-            q_out = torch.empty((tokens, heads, dim), dtype=k.dtype, device=k.device)
+            q_out = k.new_empty(shape)
+            op = q_out.data_ptr()
+        else:
+            op = _on_gpu(q_out, dtype, shape, "q_out")
     half = inv_freq.numel()
-    code = library().rm_rotary_append(
-        kind, c, s, heads, qp, qs, qh, kp, ks, kh, vp, vs, vh,
-        _on_gpu(positions, torch.int32, (tokens,), "positions"),
+    code = (_lib or library()).rm_rotary_append(
+        kind, c, s, heads, qp, qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0],
+        vs[1], _on_gpu(positions, torch.int32, (tokens,), "positions"),
         _on_gpu(inv_freq, torch.float32, (half,), "inv_freq"), 2 * half,
-        _named(ROTARY_NAMES, layout, "layout"), rot_scale,
-        _on_gpu(q_out, k.dtype, (tokens, heads, dim), "q_out"),
-        _on_gpu(status, torch.int32, (1,), "status"), _raw_stream(k))
+        _named(ROTARY_NAMES, layout, "layout"), rot_scale, op,
+        _on_gpu(status, torch.int32, (1,), "status"), _raw_stream(k.get_device()))
     if code:
         _check(code, "rm_rotary_append")
     return q_out
@@ -577,14 +588,15 @@ def rm_cache_read(cache, pages, dtype=torch.bfloat16, status=None):
     page_tokens, kv_heads, head_dim]."""
     c = _cache_of(cache)
     n = pages.numel()
-    if dtype not in TYPES:
+    kind = TYPES.get(dtype)
+    if kind is None:
         raise ValueError(f"dtype: expected bfloat16 or float16, got {dtype}")
-    k, v = (torch.empty((n, c.page_tokens, c.kv_heads, c.head_dim), dtype=dtype,
-                        device=pages.device) for _ in range(2))
-    code = library().rm_cache_read(TYPES[dtype], c, n,
-                                   _on_gpu(pages, torch.int32, (n,), "pages"), k.data_ptr(),
-                                   v.data_ptr(), _on_gpu(status, torch.int32, (1,), "status"),
-                                   _raw_stream(pages))
+    both = torch.empty((2, n, c.page_tokens, c.kv_heads, c.head_dim), dtype=dtype,
+                       device=pages.device)
+    k, v = both.unbind()
+    code = (_lib or library()).rm_cache_read(
+        kind, c, n, _on_gpu(pages, torch.int32, (n,), "pages"), k.data_ptr(), v.data_ptr(),
+        _on_gpu(status, torch.int32, (1,), "status"), _raw_stream(pages.get_device()))
     if code:
         _check(code, "rm_cache_read")
     return k, v
@@ -594,26 +606,28 @@ def rm_cache_attention(q, cache, table, lengths, token_offsets=None, max_tokens=
                        window=0, workspace=None, out=None, status=None):
     """Attention of q [tokens, heads, dim] over the cache (causal; `window` > 0
     keeps each token's last `window`).  scale None: 1 / sqrt(dim)."""
-    kind = _type_of(q, "q")
+    kind, dtype = _type_of(q, "q"), q.dtype
     c = _cache_of(cache)
     if q.dim() != 3:
         raise ValueError("q: expected [tokens, heads, head_dim]")
-    tokens, heads = q.shape[0], q.shape[1]
-    shape = (tokens, heads, c.head_dim)
-    qp, qs, qh = _rows(q, q.dtype, shape, "q")
+    tokens, heads, dim = shape = q.shape
+    qs = _rows(q, dtype, (tokens, heads, c.head_dim), "q")
     s = _sequences_of(table, lengths, token_offsets, tokens, max_tokens)
-    lib = library()
+    lib = _lib or library()
     if workspace is None:
         need = lib.rm_cache_attention_workspace_bytes(c, s, heads)
         if need == 0:
             raise ValueError("rm_cache_attention: invalid sizes or options")
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     if out is None:
-        out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        out = q.new_empty(shape)
+        op = out.data_ptr()
+    else:
+        op = _on_gpu(out, dtype, shape, "out")
     code = lib.rm_cache_attention(
-        kind, c, s, heads, qp, qs, qh, c.head_dim ** -0.5 if scale is None else scale, window,
-        _on_gpu(out, q.dtype, shape, "out"), workspace.data_ptr(), workspace.numel(),
-        _on_gpu(status, torch.int32, (1,), "status"), _raw_stream(q))
+        kind, c, s, heads, q.data_ptr(), qs[0], qs[1], dim ** -0.5 if scale is None else scale,
+        window, op, workspace.data_ptr(), workspace.numel(),
+        _on_gpu(status, torch.int32, (1,), "status"), _raw_stream(q.get_device()))
     if code:
         _check(code, "rm_cache_attention")
     return out
@@ -625,32 +639,42 @@ def rm_norm_residual(x, y=None, gate=None, post_weight=None, pre_weight=None, pr
     where that is given; n = x' normalised times pre_weight plus pre_bias.
     x, y [rows, width]; gate [width], [rows, 1] or [rows, width].  Without y
     x' is x itself."""
-    code_type = _type_of(x, "x")
+    code_type, dtype = _type_of(x, "x"), x.dtype
     if x.dim() != 2:
         raise ValueError("x: expected [rows, width]")
     rows, width = shape = x.shape
-    xp, xs = _rows(x, x.dtype, shape, "x")
-    yp, ys = _rows(y, x.dtype, shape, "y") if y is not None else (None, 0)
+    x_pitch = _pitch(_rows(x, dtype, shape, "x")[0], rows, width, "x")
+    yp, y_pitch = None, 0
+    if y is not None:
+        y_pitch = _pitch(_rows(y, dtype, shape, "y")[0], rows, width, "y")
+        yp = y.data_ptr()
     gp, gs, gw = None, 0, 0
     if gate is not None:
         if gate.dim() == 1:
-            gp, gw = _on_gpu(gate, x.dtype, (width,), "gate"), width
+            gp, gw = _on_gpu(gate, dtype, (width,), "gate"), width
         else:
             gw = gate.shape[1]
-            gp, gs = _rows(gate, x.dtype, (rows, gw), "gate")
-            gs = gs if rows > 1 else 0
+            gs = _rows(gate, dtype, (rows, gw), "gate")[0] if rows > 1 else 0
+            gp = gate.data_ptr() if rows > 1 else _on_gpu(gate, dtype, (rows, gw), "gate")
     if x_out is None:
-        x_out = x if y is None else torch.empty(shape, dtype=x.dtype, device=x.device)
+        if y is None:
+            x_out, xo = x, None
+        else:
+            x_out = x.new_empty(shape)
+            xo = x_out.data_ptr()
+    else:
+        xo = _on_gpu(x_out, dtype, shape, "x_out")
     if n_out is None:
-        n_out = torch.empty(shape, dtype=x.dtype, device=x.device)
-    code = library().rm_norm_residual(
-        code_type, _named(NORM_NAMES, kind, "kind"), rows, width, xp,
-        _pitch(xs, rows, width, "x"), yp, _pitch(ys, rows, width, "y") if yp else 0, gp,
-        gs, gw, _on_gpu(post_weight, x.dtype, (width,), "post_weight"),
-        _on_gpu(pre_weight, x.dtype, (width,), "pre_weight"),
-        _on_gpu(pre_bias, x.dtype, (width,), "pre_bias"), alpha, eps,
-        None if x_out is x and y is None else _on_gpu(x_out, x.dtype, shape, "x_out"),
-        _on_gpu(n_out, x.dtype, shape, "n_out"), _raw_stream(x))
+        n_out = x.new_empty(shape)
+        no = n_out.data_ptr()
+    else:
+        no = _on_gpu(n_out, dtype, shape, "n_out")
+    wide = (width,)
+    code = (_lib or library()).rm_norm_residual(
+        code_type, _named(NORM_NAMES, kind, "kind"), rows, width, x.data_ptr(), x_pitch, yp,
+        y_pitch, gp, gs, gw, _on_gpu(post_weight, dtype, wide, "post_weight"),
+        _on_gpu(pre_weight, dtype, wide, "pre_weight"), _on_gpu(pre_bias, dtype, wide, "pre_bias"),
+        alpha, eps, xo, no, _raw_stream(x.get_device()))
     if code:
         _check(code, "rm_norm_residual")
     return x_out, n_out
