@@ -164,9 +164,6 @@ struct Packing {
 // Fills `pk`; false when W > 127 or the fields need more than 56 bits.
 bool make_packing(const Desc& d, Packing* pk);
 
-// Keeps a HIP error's name for rm_status_string; RM_ELAUNCH.
-int launch_failed(hipError_t e);
-
 // ---- launchers (defined next to their kernels) ----------------------------
 // Each returns the hipError_t of its launch.
 

@@ -11,6 +11,9 @@
 
 namespace rm {
 
+// Keeps a HIP error's name for rm_status_string (api.hip); RM_ELAUNCH.
+int launch_failed(hipError_t e);
+
 typedef __bf16 bf16;
 typedef _Float16 f16;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
