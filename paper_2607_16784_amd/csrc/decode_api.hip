@@ -29,9 +29,9 @@ bool type_ok(int32_t type)
 // RM_OK, or what is wrong with a cache.
 int check_cache(const rm_cache* c)
 {
-    if (!c || c->n_pages < 1 || c->kv_heads < 1) return RM_EINVAL;
+    if (!c || c->n_pages < 0 || c->kv_heads < 1) return RM_EINVAL;
     if (c->codes != RM_CODES_INT8 && c->codes != RM_CODES_E4M3) return RM_EINVAL;
-    if (!c->k || !c->v || !c->k_scale || !c->v_scale) return RM_EINVAL;
+    if (c->n_pages > 0 && (!c->k || !c->v || !c->k_scale || !c->v_scale)) return RM_EINVAL;
     // the kernels read and write codes 16 bytes at a time
     if (((uintptr_t)c->k | (uintptr_t)c->v) & 15) return RM_EINVAL;
     const int32_t t = c->page_tokens, d = c->head_dim;
@@ -128,6 +128,7 @@ int rm_rotary_append(int32_t type, const rm_cache* cache, const rm_sequences* se
     if (layout != RM_ROTARY_HALF && layout != RM_ROTARY_INTERLEAVED) return RM_EINVAL;
     if (heads > 65535) return RM_EUNSUPPORTED;
     if (seqs->n_tokens == 0) return RM_OK;
+    if (cache->n_pages < 1) return RM_EINVAL;
     if (!k || !v || (heads > 0 && (!q || !q_out)) || (rot > 0 && !inv_freq)) return RM_EINVAL;
     rm::AppendArgs a = {*cache, *seqs, heads, rot, layout, q, k, v, q_stride, q_head_stride,
                         k_stride, k_head_stride, v_stride, v_head_stride, positions, inv_freq,
@@ -142,7 +143,7 @@ int rm_cache_read(int32_t type, const rm_cache* cache, int32_t n, const int32_t*
     if (e != RM_OK) return e;
     if (!rm::type_ok(type) || n < 0) return RM_EINVAL;
     if (n == 0) return RM_OK;
-    if (!pages || !k || !v) return RM_EINVAL;
+    if (!pages || !k || !v || cache->n_pages < 1) return RM_EINVAL;
     return rm::done(rm::launch_cache_read(type, *cache, n, pages, k, v, status,
                                           (hipStream_t)stream));
 }
@@ -167,7 +168,7 @@ int rm_cache_attention(int32_t type, const rm_cache* cache, const rm_sequences* 
         !std::isfinite(scale))
         return RM_EINVAL;
     if (seqs->n_tokens == 0) return RM_OK;
-    if (!q || !out) return RM_EINVAL;
+    if (!q || !out || cache->n_pages < 1) return RM_EINVAL;
     const size_t need = rm::attend_workspace(*cache, *seqs, heads);
     if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255))
         return RM_EWORKSPACE;
