@@ -27,6 +27,9 @@ namespace {
 constexpr int kBlock = 64;    // cached tokens a wave takes at a time
 constexpr int kWaves = 4;
 constexpr int kMostSplits = 256;
+// Weights and their sums carry 2^kLift, which the quotient takes off again: f16
+// holds weights in full down to 2^-28 of the largest, below that to 2^-39.
+constexpr float kLift = 14.0f;
 
 __device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c)
 {
@@ -250,8 +253,9 @@ attend_kernel(AttendArgs a, Plan plan)
         // while its keys are multiplied, and the page after it is looked up
         __builtin_amdgcn_sched_barrier(0);         // the codes stay codes until their turn
         const float k_log2 = ks * to_log2;
-        const bool bad = now.bad;
-        if (bad) st = RM_ST_BAD_PAGE;
+        // the lane's 16 tokens share a page; one that no row sees has no say
+        const bool near = tv < t.hi && tv + 16 > t.lo, bad = now.bad;
+        if (bad && near) st = RM_ST_BAD_PAGE;
         next = checked(next);
         load_k(following, next);
         const Pages after = ids(min(following + W, upto - 1));
@@ -279,8 +283,10 @@ attend_kernel(AttendArgs a, Plan plan)
             top[c] = fmaxf(m[c], rows_reduce<Max>(x));
             moved |= top[c] > m[c];
         }
-        const float v_scale = vs;
-        const float largest = fmaxf(ref, rows_reduce<Max>(bad ? 0.0f : v_scale));
+        // a scale that is not finite goes into the weights as it is and reaches
+        // the rows that see the page, not the common factor
+        const float v_scale = near && !bad ? vs : 0.0f;
+        const float largest = fmaxf(ref, rows_reduce<Max>(v_scale < INFINITY ? v_scale : 0.0f));
         if (__any(moved || largest > ref)) {
             const float shrink = largest > 0.0f ? ref / largest : 1.0f;
 #pragma unroll
@@ -293,11 +299,11 @@ attend_kernel(AttendArgs a, Plan plan)
             }
             ref = largest;
         }
-        const float share = ref > 0.0f ? v_scale / ref : 0.0f;
+        const float share = v_scale / (ref > 0.0f ? ref : 1.0f);
         f16x8 p[2][C];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const float base = m[c] == -INFINITY ? 0.0f : m[c];
+            const float base = m[c] == -INFINITY ? 0.0f : m[c] - kLift;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll

@@ -159,6 +159,63 @@ def test_what_is_not_seen_may_hold_anything(codes):
     check(api.rm_cache_attention(q, cache, table, lens, **kw), want, size, cache, lengths)
 
 
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("window", [0, 24])
+def test_scales_that_are_not_finite_stay_with_the_rows_that_see_them(bad, window):
+    # a chunk whose rows end in different pages: one page's scales spoil the
+    # rows that see it and no others
+    length, new = 90, 60
+    cache, table, lens, _ = make_cache([length], 2, 16, 64, INT8, 71)
+    q = torch.randn((new, 4, 64), device="cuda").bfloat16()
+    kw = dict(token_offsets=torch.tensor([0, new], dtype=torch.int32, device="cuda"),
+              max_tokens=new, window=window)
+    want, size = ref.attention(q, cache, table, [length], [0, new], None, window)
+    for page in range(6):
+        for name in ("k_scale", "v_scale"):
+            c = {n: t.clone() for n, t in cache.items()}
+            c[name][int(table[0, page])] = bad
+            got = api.rm_cache_attention(q, c, table, lens, **kw)
+            pos = torch.arange(length - new, length)
+            sees = (pos >= page * 16) & ((pos - window < page * 16 + 15) | (window == 0))
+            free = (~sees).nonzero()[:, 0]
+            check(got[free], want[free], size[free], cache, [length])
+            # codes of 0 and +inf of the wrong sign aside, a seen one shows
+            assert not torch.isfinite(got.cpu()[sees]).all() or not sees.any()
+
+
+def test_small_weights_beside_a_large_one():
+    # 4000 weights of 2^-20 to 2^-22 of the largest one: together 10^-3 of the
+    # sum, on values that are all alike and 100 times the large one's
+    cache, table, lens, _ = make_cache([4001], 1, 64, 64, INT8, 72)
+    cache["k"].zero_()
+    cache["v"].fill_(100)
+    cache["k_scale"].fill_(1.0)
+    cache["v_scale"].fill_(1.0)
+    cache["k"][int(table[0, 5]), 0, 7, 0] = 112
+    cache["v"][int(table[0, 5]), 0, :, 7] = 1
+    q = torch.zeros((1, 1, 64), device="cuda").half()
+    q[0, 0, 0] = 1.0
+    w = 1 / (4000 * 2.718281828459045 ** -14 + 1)        # 112 / 8
+    want = w * 1 + (1 - w) * 100
+    got = api.rm_cache_attention(q, cache, table, lens).double()
+    # f16 rounding of the output and of the weights, 2^-11 each
+    assert float((got - want).abs().max()) < 2.0 ** -10 * want
+
+
+def test_pages_that_no_row_sees_are_not_reported():
+    cache, table, lens, _ = make_cache([200], 2, 16, 64, INT8, 73)
+    q = torch.randn((1, 4, 64), device="cuda").bfloat16()
+    want = api.rm_cache_attention(q, cache, table, lens, window=20)
+    st = api.new_status()
+    t = table.clone()
+    t[0, :11] = -1                       # tokens 180 and later are seen
+    got = api.rm_cache_attention(q, cache, t, lens, window=20, status=st)
+    assert int(st.item()) == 0 and torch.equal(got, want)
+    t[0, 11] = -1
+    api.rm_cache_attention(q, cache, t, lens, window=20, status=st)
+    assert int(st.item()) == api.ST_BAD_PAGE
+
+
 def test_sequences_without_tokens_and_out_of_range():
     cache, table, lens, _ = make_cache([20, 40, 30, 50], 2, 16, 64, INT8, 66)
     q = torch.randn((4, 4, 64), device="cuda").bfloat16()
