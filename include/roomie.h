@@ -122,6 +122,8 @@ extern "C" {
 
 #define RM_MAX_NORM_WIDTH    32768  /* width of rm_norm_residual               */
 #define RM_MAX_W4_COLUMNS  2097152  /* k of rm_w4_linear                       */
+#define RM_MAX_W4_OUTPUTS 1073741824 /* n of rm_w4_linear                      */
+#define RM_MAX_W4_ROWS     4194240  /* rows of rm_w4_linear                    */
 #define RM_MAX_SEQUENCES     65535  /* n_seqs of the cache calls               */
 
 /* Target-device descriptor: the SM limits of Eq. (1) and Eq. (2).
@@ -523,7 +525,8 @@ typedef struct {
  *   none, workspace may be NULL).  The order of every sum is fixed.
  * Errors: RM_EINVAL (NULL pointer, rows < 0, n or k < 1, a stride below its
  *   row, group not a multiple of 32, SWIGLU with odd n, bad type or act),
- *   RM_EUNSUPPORTED (k > RM_MAX_W4_COLUMNS), RM_EWORKSPACE, RM_ELAUNCH.
+ *   RM_EUNSUPPORTED (k > RM_MAX_W4_COLUMNS, n > RM_MAX_W4_OUTPUTS, rows >
+ *   RM_MAX_W4_ROWS), RM_EWORKSPACE, RM_ELAUNCH.
  */
 size_t rm_w4_linear_workspace_bytes(int32_t rows, int32_t n, int32_t k, int32_t act);
 int rm_w4_linear(int32_t type, int32_t rows, int32_t n, int32_t k, const void* x,
@@ -546,8 +549,9 @@ int rm_w4_linear(int32_t type, int32_t rows, int32_t n, int32_t k, const void* x
  * A page and head that gets new tokens: scale = max(scale of its older tokens,
  * largest new magnitude / Q), Q = 127 or 448; older codes become
  * round(code * old scale / scale), new ones round(value / scale) (ties to
- * even), and the slots behind the last token 0.  A non-finite value makes the page's scale, and so all that
- * the head reads from the page, not finite.
+ * even), and the slots behind the last token 0.  Where no new magnitude passes
+ * 1e-36 the new codes may be 0.  A non-finite value makes the page's scale, and
+ * so all that the head reads from the page, not finite.
  * No page may be in two of the call's sequences where tokens are appended.
  * heads may be 0 (q and q_out are then not read).
  * Errors: RM_EINVAL (NULL pointer, negative size, rot odd or > head_dim, bad
@@ -581,9 +585,14 @@ int rm_cache_read(int32_t type, const rm_cache* cache, int32_t n, const int32_t*
  * statistics and sums are fp32; a cached code is exact in the product's type;
  * the softmax weights enter the second product as f16 times the scale of the
  * values' page, relative to the largest such scale so far.
+ * Tokens that a row does not see do not reach it, whatever their codes and
+ * scales hold, with one exception: a value code that is e4m3's NaN (the append
+ * writes none) reaches all of a call's own tokens of that sequence and head.
+ * A page id out of range is reported where some token sees the page.
  * workspace: rm_cache_attention_workspace_bytes bytes, 256-byte aligned.
  * Errors: RM_EINVAL (also heads not a multiple of kv_heads, scale not finite,
- *   window < 0), RM_EUNSUPPORTED, RM_EWORKSPACE, RM_ELAUNCH.
+ *   window < 0), RM_EUNSUPPORTED (also max_tokens * heads / kv_heads beyond 31
+ *   bits), RM_EWORKSPACE, RM_ELAUNCH.
  */
 size_t rm_cache_attention_workspace_bytes(const rm_cache* cache, const rm_sequences* seqs,
                                           int32_t heads);

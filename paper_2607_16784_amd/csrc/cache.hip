@@ -309,7 +309,8 @@ __global__ __launch_bounds__(1024) void append_kernel(AppendArgs a, int32_t q_bl
     // quotient halfway between two codes comes out halfway
     const bool raised = !(now == was);
     const float num = raised ? Q : 1.0f, den = raised ? top : was;
-    const float inv = den > 0.0f ? 1.0f / den : 0.0f;
+    // magnitudes below 1e-36, whose reciprocal times Q is no number, count as 0
+    const float inv = den > 0.0f && Q / den < INFINITY ? 1.0f / den : 0.0f;
     if (t == 0) scales[block] = now;                // all have read the old one
     if (!in) return;
     uint8_t* codes = static_cast<uint8_t*>(value ? a.cache.v : a.cache.k) + block * TK * D;

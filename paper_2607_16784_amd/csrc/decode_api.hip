@@ -54,12 +54,17 @@ int check_seqs(const rm_sequences* s, const rm_cache* c)
     return RM_OK;
 }
 
-// floor(k / group) = umulhi(k / 32, inverse) for every column below k: the
-// product's error, k / 32 / 2^32, stays below 32 / group for k <= 2^21 (a group
-// beyond k counts as the next multiple of 32).
-uint32_t inverse_of(int32_t k, int32_t group)
+// (token, head) pairs of a sequence and kv head are counted in 32 bits.
+bool rows_fit(const rm_sequences* s, const rm_cache* c, int32_t heads)
 {
-    const uint32_t d = (uint32_t)(group < k ? group : k + 31) / 32;
+    return (int64_t)s->max_tokens * (heads / c->kv_heads) <= 0x7fffff00;
+}
+
+// floor(k / group) = umulhi(k / 32, inverse) for every column below k: the
+// product's error, k / 32 / 2^32, stays below 32 / group for k <= 2^21.
+uint32_t inverse_of(int32_t group)
+{
+    const uint32_t d = (uint32_t)group / 32;
     return d <= 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + d - 1) / d);
 }
 
@@ -87,7 +92,9 @@ extern "C" {
 
 size_t rm_w4_linear_workspace_bytes(int32_t rows, int32_t n, int32_t k, int32_t act)
 {
-    if (rows < 1 || n < 1 || k < 1 || k > RM_MAX_W4_COLUMNS) return 0;
+    if (rows < 1 || n < 1 || k < 1 || k > RM_MAX_W4_COLUMNS || n > RM_MAX_W4_OUTPUTS ||
+        rows > RM_MAX_W4_ROWS)
+        return 0;
     return rm::linear_workspace(rows, n, k, act);
 }
 
@@ -102,14 +109,17 @@ int rm_w4_linear(int32_t type, int32_t rows, int32_t n, int32_t k, const void* x
     if (act == RM_ACT_SWIGLU && n % 2) return RM_EINVAL;
     const int32_t out = act == RM_ACT_SWIGLU ? n / 2 : n;
     if (x_stride < k || code_stride < (k + 1) / 2 || y_stride < out) return RM_EINVAL;
-    if (k > RM_MAX_W4_COLUMNS) return RM_EUNSUPPORTED;
+    if (k > RM_MAX_W4_COLUMNS || n > RM_MAX_W4_OUTPUTS || rows > RM_MAX_W4_ROWS)
+        return RM_EUNSUPPORTED;
+    // a group beyond k is the one group of k: sums of sizes stay within 32 bits
+    if (group > k) group = (k + 31) / 32 * 32;
     if (rows == 0) return RM_OK;
     if (!x || !codes || !scales || !y) return RM_EINVAL;
     const size_t need = rm::linear_workspace(rows, n, k, act);
     if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255)))
         return RM_EWORKSPACE;
-    rm::LinearArgs a = {rows, n, k, group, x, codes, scales, zeros, bias, y, workspace, rm::inverse_of(k, group), x_stride,
-                        code_stride, y_stride};
+    rm::LinearArgs a = {rows, n, k, group, x, codes, scales, zeros, bias, y, workspace,
+                        rm::inverse_of(group), x_stride, code_stride, y_stride};
     return rm::done(rm::launch_linear(type, act, a, (hipStream_t)stream));
 }
 
@@ -152,7 +162,7 @@ size_t rm_cache_attention_workspace_bytes(const rm_cache* cache, const rm_sequen
                                           int32_t heads)
 {
     if (rm::check_cache(cache) != RM_OK || rm::check_seqs(seqs, cache) != RM_OK) return 0;
-    if (heads < 1 || heads % cache->kv_heads) return 0;
+    if (heads < 1 || heads % cache->kv_heads || !rm::rows_fit(seqs, cache, heads)) return 0;
     return rm::attend_workspace(*cache, *seqs, heads);
 }
 
@@ -167,6 +177,7 @@ int rm_cache_attention(int32_t type, const rm_cache* cache, const rm_sequences* 
     if (!rm::type_ok(type) || heads < 1 || heads % cache->kv_heads || window < 0 ||
         !std::isfinite(scale))
         return RM_EINVAL;
+    if (!rm::rows_fit(seqs, cache, heads)) return RM_EUNSUPPORTED;
     if (seqs->n_tokens == 0) return RM_OK;
     if (!q || !out || cache->n_pages < 1) return RM_EINVAL;
     const size_t need = rm::attend_workspace(*cache, *seqs, heads);

@@ -40,6 +40,8 @@ def test_w4_linear(lib):
                dict(x=None), dict(codes=None), dict(scales=None), dict(y=None)):
         assert call(**kw) == 1, kw
     assert call(k=1 << 25, xs=1 << 25, cs=1 << 24) == 3
+    assert call(n=(1 << 30) + 1, ys=1 << 31) == 3
+    assert call(rows=1 << 23) == 3 and lib.rm_w4_linear_workspace_bytes(1 << 23, 8, 64, 0) == 0
     # sizes whose columns are split need a workspace
     big = dict(rows=64, n=512, k=8192, xs=8192, cs=4096, ys=512)
     need = lib.rm_w4_linear_workspace_bytes(64, 512, 8192, 0)
@@ -100,6 +102,13 @@ def test_cache_attention(lib):
         assert call(c=cache(**kw)) == code, kw
     for kw, code in BAD_SEQS:
         assert call(s=seqs(**kw)) == code, kw
+
+
+def test_rows_of_a_sequence_beyond_31_bits(lib):
+    s = seqs(max_tokens=1 << 30)
+    assert lib.rm_cache_attention(0, cache(), s, 4, P, 64, 64, 1.0, 0, P, P, 1 << 60, None,
+                                  None) == 3
+    assert lib.rm_cache_attention_workspace_bytes(cache(), s, 4) == 0
 
 
 def test_cache_attention_workspace(lib):

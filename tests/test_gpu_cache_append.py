@@ -133,6 +133,24 @@ def test_tokens_one_at_a_time_and_all_zero():
         assert torch.all(v[0, n:] == 0)
 
 
+@pytest.mark.parametrize("codes", [INT8, E4M3], ids=["int8", "e4m3"])
+def test_magnitudes_without_a_reciprocal(codes):
+    # bf16 holds numbers whose reciprocal is beyond fp32: what is 0 stays 0 and
+    # nothing is read back larger than it was, behind older zeros too
+    cache = api.new_cache(2, 1, 16, 64, codes)
+    table = torch.tensor([[1]], dtype=torch.int32, device="cuda")
+    x = torch.zeros((3, 1, 64), dtype=torch.bfloat16, device="cuda")
+    x[0, 0, ::2], x[2, 0, 1::2] = 1e-39, -3e-38
+    for n in range(3):
+        api.rm_rotary_append(None, x[n:n + 1], x[n:n + 1], torch.zeros(0, device="cuda"), cache,
+                             table, torch.tensor([n + 1], dtype=torch.int32, device="cuda"))
+        for name in ("k", "v"):
+            c = cache[name].float() * cache[name + "_scale"][..., None, None]
+            c = (c if name == "k" else c.transpose(2, 3))[1, 0, :n + 1]
+            assert torch.all(c[x[:n + 1, 0] == 0] == 0)
+            assert torch.all((c - x[:n + 1, 0].float()).abs() <= 3.1e-38)
+
+
 def test_positions_beyond_a_million_keep_their_angle():
     pos = [0, 1, 65535, 1000003, 2 ** 31 - 1]
     run([5], [5], 2, 1, 16, 64, INT8, torch.float16, 64, "half", seed=31, positions=pos)

@@ -156,6 +156,16 @@ def test_refusals():
             call()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows", [1, 16, 40])
+def test_a_group_of_any_size_beyond_k_is_one_group(rows, dtype):
+    x, codes, scales, z, b = inputs(rows, 96, 1100, 1120, dtype, True, True, seed=95)
+    want = api.rm_w4_linear(x, codes, scales, 1120, zeros=z, bias=b)
+    check(x, codes, scales, 1120, z, b, "none", want)
+    for group in (1 << 20, (1 << 31) - 32):
+        assert torch.equal(api.rm_w4_linear(x, codes, scales, group, zeros=z, bias=b), want)
+
+
 def test_no_rows():
     x, codes, scales, z, b = inputs(2, 8, 64, 32, torch.bfloat16, False, False, seed=9)
     assert api.rm_w4_linear(x[:0], codes, scales, 32).shape == (0, 8)
