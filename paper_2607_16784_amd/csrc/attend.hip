@@ -494,9 +494,10 @@ Plan plan_of(const rm_cache& c, const rm_sequences& s, int32_t heads)
     // Two workgroups a CU, as far as every wave has two blocks of the longest
     // possible sequence.  One sequence of 501 tokens: 10.9 us in one part, 11.6 in
     // two; two of 125 000: 108 us in 32 parts, 115 in 64; 64 ragged ones of up to
-    // 4096, 512 workgroups already: 68 us, in two parts 84.
+    // 4096, 512 workgroups already: 65 us, in two parts 69; 40 ragged ones of up to
+    // 16 000, 320 workgroups: 269 us in one part, 183 in two.
     const int64_t blocks = ((int64_t)s.table_stride * c.page_tokens + kBlock - 1) / kBlock;
-    const int64_t want = units > 0 ? 2 * kComputeUnits / units : 1;
+    const int64_t want = units > 0 ? (2 * kComputeUnits + units - 1) / units : 1;
     const int64_t most = blocks / (2 * kWaves);
     p.splits = (int32_t)(want < most ? want : most);
     if (p.splits > kMostSplits) p.splits = kMostSplits;
