@@ -672,7 +672,7 @@ hipError_t launch_many(const LinearArgs& a, int parts_z, hipStream_t s)
 
 // What is taken for which sizes; us at the sizes named, measured one after the
 // other on buffers that rotate through 3 copies.
-enum Kind { kRows, kRowsWide, kTile, kTile2, kTile4 };
+enum Kind { kRows, kRowsWide, kTile, kTile2, kTile2Tall, kTile4 };
 struct Plan {
     Kind kind;
     int parts_z;
@@ -713,6 +713,10 @@ Plan plan_of(int32_t rows, int32_t n, int32_t k, int act)
     p.parts_z = (int)(want < most ? want : most);
     if (p.parts_z > 8) p.parts_z = 8;
     if (p.parts_z < 1) p.parts_z = 1;
+    // 64 rows of x a workgroup where that fills the CUs (64 x 8192 x 28672: 81 us
+    // in a graph, 32 rows 97), else 32 (64 x 4096 x 14336 in groups of 32: 44 us, 64
+    // rows 80; 48 x 6000 x 5000: 29 and 35; 128 x 4096 x 4096: 21 and 27)
+    if (p.kind == kTile4 && blocks * p.parts_z < kComputeUnits) p.kind = kTile2Tall;
     return p;
 }
 
@@ -726,6 +730,7 @@ hipError_t launch_rows(const LinearArgs& a, hipStream_t s)
     case kRowsWide: return launch_few<T, ONE, PER, ACT, 2, 4, 2>(a, 1, 64 * 1024, s);
     case kTile: return launch_many<T, 2, 1, PER, ACT, 2, 4, 2, 2>(a, p.parts_z, s);
     case kTile2: return launch_many<T, 2, 2, PER, ACT, 1, 4, 2, 2>(a, p.parts_z, s);
+    case kTile2Tall: return launch_many<T, 2, 2, PER, ACT, 1, 8, 1, 2>(a, p.parts_z, s);
     default: return launch_many<T, 2, 4, PER, ACT, 1, 8, 1, 2>(a, p.parts_z, s);
     }
 }

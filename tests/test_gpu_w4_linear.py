@@ -69,6 +69,10 @@ CASES = [
     (64, 300, 4100, 32, True, True, "none"),
     (61, 260, 9216, 128, True, False, "swiglu"),
     (200, 270, 2600, 64, False, True, "none"),
+    # 64 rows a workgroup, in one part of the columns and in eight
+    (40, 65550, 160, 64, True, False, "none"),
+    (61, 65540, 140, 32, False, True, "swiglu"),
+    (33, 8200, 8300, 128, True, False, "none"),
 ]
 
 
