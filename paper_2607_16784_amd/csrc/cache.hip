@@ -1,9 +1,9 @@
 // cache.hip -- rotary positions with the append to the paged 8-bit cache
 // (rm_rotary_append) and the read-back of pages (rm_cache_read).
 //
-// Append, one launch: the first workgroups turn the queries, a wave a token, the
-// others own each one (page, kv head, keys or values) that gets new tokens, so no two
-// write the same codes and no atomic is needed.  A thread holds 4 tokens x 8
+// Append, one launch: the first workgroups turn the queries, a wave or more a
+// token, the others own each one (page, kv head, keys or values) that gets new
+// tokens, so no two write the same codes and no atomic is needed.  A thread holds 4 tokens x 8
 // channels in registers: the tile that makes both sides of the page wide, 8
 // consecutive key codes a token and 4 consecutive tokens a value channel.  A
 // page's old codes are read only where a new token raises the scale; the rest
@@ -30,8 +30,8 @@ __device__ inline double turns_of(const float* inv_freq, int pair)
 // Sine and cosine of position * turns whole turns, times scale.  What is left
 // of the last turn goes through v_sin_f32 and v_cos_f32, which take turns: off
 // by up to 1.3e-7 over [-1/2, 1/2] (measured), against 5e-8 of sincospif, whose
-// instructions bound the prompts' append (7600 tokens: 47.5 us, 40.3 so, 35.2
-// without any angle).
+// instructions bound the prompts' append (7600 tokens, the same again and again:
+// 47.5 us, 40.3 so, 35.2 without any angle; 52 with inputs that change).
 __device__ inline void turn_of(double turns, int32_t position, float scale, float& cs, float& sn)
 {
     const double a = (double)position * turns;
@@ -131,10 +131,13 @@ __device__ inline float decode_byte(uint32_t byte)
     return __builtin_amdgcn_cvt_f32_fp8((int)byte, 0);
 }
 
-// The queries of one token, by one wave: 4 pairs a lane and head, the token's
-// sines and cosines in the wave's LDS.
+constexpr int kAhead = 4;         // units of 4 pairs that a lane has in flight
+
+// The queries of one token, by `parts` waves of which this is number `part`: 4
+// pairs a lane and head, the token's sines and cosines in the wave's LDS.
 template <typename T>
-__device__ inline void turn_queries(const AppendArgs& a, int32_t token, float2* turn)
+__device__ inline void turn_queries(const AppendArgs& a, int32_t token, int part, int parts,
+                                    float2* turn)
 {
     typedef typename Vec<T>::x8 V;
     const int lane = threadIdx.x & 63, half = a.rot >> 1, D = a.cache.head_dim;
@@ -145,10 +148,10 @@ __device__ inline void turn_queries(const AppendArgs& a, int32_t token, float2* 
         load_pairs(q + u / units * a.q_head, u % units * 4, a.rot, a.layout, wide, v);
     };
     // the first turns' queries are on their way while the token is placed
-    constexpr int AHEAD = 4;
-    float ahead[AHEAD][8];
+    const int begin = part * (kAhead * 64) + lane;
+    float ahead[kAhead][8];
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) load(min(lane + i * 64, all - 1), ahead[i]);
+    for (int i = 0; i < kAhead; ++i) load(min(begin + i * 64, all - 1), ahead[i]);
     int32_t position = 0;
     if (a.positions) {
         position = a.positions[token];
@@ -197,27 +200,29 @@ __device__ inline void turn_queries(const AppendArgs& a, int32_t token, float2* 
             }
         }
     };
-    for (int u0 = lane; u0 - lane < all; u0 += AHEAD * 64) {
-        if (u0 != lane) {
+    for (int u0 = begin; u0 - lane < all; u0 += parts * (kAhead * 64)) {
+        if (u0 != begin) {
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i) load(min(u0 + i * 64, all - 1), ahead[i]);
+            for (int i = 0; i < kAhead; ++i) load(min(u0 + i * 64, all - 1), ahead[i]);
         }
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
+        for (int i = 0; i < kAhead; ++i)
             if (u0 + i * 64 < all) finish(u0 + i * 64, ahead[i]);
     }
 }
 
 template <typename T, int FMT>
 __global__ __launch_bounds__(1024) void append_kernel(AppendArgs a, int32_t q_blocks,
-                                                      int32_t pages_a_seq, int32_t group)
+                                                      int32_t q_parts, int32_t pages_a_seq,
+                                                      int32_t group)
 {
     __shared__ float2 turn[16][kMostPairs];
     __shared__ float part[16];
     if ((int)blockIdx.x < q_blocks) {
         const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-        const int64_t token = (int64_t)blockIdx.x * waves + wave;
-        if (token < a.seqs.n_tokens) turn_queries<T>(a, (int32_t)token, turn[wave]);
+        const int64_t at = (int64_t)blockIdx.x * waves + wave, token = at / q_parts;
+        if (token < a.seqs.n_tokens)
+            turn_queries<T>(a, (int32_t)token, (int)(at % q_parts), q_parts, turn[wave]);
         return;
     }
     // `group` threads a (page, head, side); the groups of a workgroup share
@@ -456,15 +461,23 @@ hipError_t launch_append(int type, const AppendArgs& a, hipStream_t s)
     const int tile = TK * a.cache.head_dim / 32;
     const int group = tile < 64 ? 64 : tile, threads = group < 256 ? 256 : group;
     const int groups = threads / group, waves = threads / 64;
-    const int32_t q_blocks = a.heads > 0 ? (a.seqs.n_tokens + waves - 1) / waves : 0;
+    // Waves a token: as many as its queries fill once, while all are 16 a CU at
+    // most (17 tokens of 64 heads of 256, with the read back: 10.6 us, a wave a
+    // token 31.6; 64 tokens of 32 heads of 128: 10.1 and 12.0).
+    const int64_t fill = ((int64_t)a.heads * (a.cache.head_dim / 8) + kAhead * 64 - 1) /
+                         (kAhead * 64);
+    const int64_t room = 16 * kComputeUnits / a.seqs.n_tokens;
+    const int32_t q_parts = (int32_t)(room < 1 ? 1 : room < fill ? room : fill < 1 ? 1 : fill);
+    const int64_t q_blocks = a.heads > 0 ? ((int64_t)a.seqs.n_tokens * q_parts + waves - 1) / waves
+                                         : 0;
     const int64_t per_page = (2 * (int64_t)a.cache.kv_heads + groups - 1) / groups;
     const int64_t blocks = q_blocks + (int64_t)a.seqs.n_seqs * pages * per_page;
     if (blocks == 0) return hipSuccess;
     if (blocks > 0x7fffffff) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks);
 #define RM_APPEND(T, FMT) \
-    return launch(append_kernel<T, FMT>, grid, (unsigned)threads, 0, s, a, q_blocks, pages, \
-                  (int32_t)group)
+    return launch(append_kernel<T, FMT>, grid, (unsigned)threads, 0, s, a, (int32_t)q_blocks, \
+                  q_parts, pages, (int32_t)group)
     if (type == RM_TYPE_BF16) {
         if (a.cache.codes == RM_CODES_INT8) RM_APPEND(bf16, RM_CODES_INT8);
         RM_APPEND(bf16, RM_CODES_E4M3);

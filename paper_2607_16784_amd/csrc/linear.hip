@@ -711,7 +711,8 @@ Plan plan_of(int32_t rows, int32_t n, int32_t k, int act)
     // and 24.1 us, 32 rows 30.0 and 37.4, 64 rows 45.7 and 59.2.
     const int64_t want = (kComputeUnits + blocks / 2) / blocks, most = k / 1024;
     p.parts_z = (int)(want < most ? want : most);
-    if (p.parts_z > 8) p.parts_z = 8;
+    // 64 x 2048 x 28672: 34.6 us in sixteen parts, 51.2 in eight
+    if (p.parts_z > 16) p.parts_z = 16;
     if (p.parts_z < 1) p.parts_z = 1;
     // 64 rows of x a workgroup where that fills the CUs (64 x 8192 x 28672: 81 us
     // in a graph, 32 rows 97), else 32 (64 x 4096 x 14336 in groups of 32: 44 us, 64
