@@ -495,14 +495,15 @@ Plan plan_of(const rm_cache& c, const rm_sequences& s, int32_t heads)
     p.tiles = (int32_t)((rows + height - 1) / height);
     p.rows = (int32_t)(rows < height ? rows : height);
     const int64_t units = (int64_t)s.n_seqs * c.kv_heads * p.tiles;
-    // Two workgroups a CU, as far as every wave has two blocks of the longest
-    // possible sequence.  One sequence of 501 tokens: 10.9 us in one part, 11.6 in
-    // two; two of 125 000: 108 us in 32 parts, 115 in 64; 64 ragged ones of up to
-    // 4096, 512 workgroups already: 65 us, in two parts 69; 40 ragged ones of up to
-    // 16 000, 320 workgroups: 269 us in one part, 183 in two.
+    // Two workgroups a CU, as far as every wave has a block of the longest possible
+    // sequence and there are three each without: the join is a launch.  One sequence
+    // of 501 tokens: 9.7 us in one part, 11.0 in two; one of 2000: 11.4 in eight, 13.0
+    // in four; 26 ragged ones of up to 1457: 13.5 in five, 15.6 in two; two of 125 000:
+    // 108 in 32, 115 in 64; 64 ragged ones of up to 4096, 512 workgroups already: 65, in
+    // two parts 69; 40 of up to 16 000, 320 workgroups: 269 in one part, 183 in two.
     const int64_t blocks = ((int64_t)s.table_stride * c.page_tokens + kBlock - 1) / kBlock;
     const int64_t want = units > 0 ? (2 * kComputeUnits + units - 1) / units : 1;
-    const int64_t most = blocks / (2 * kWaves);
+    const int64_t most = blocks < 3 * kWaves ? 1 : blocks / kWaves;
     p.splits = (int32_t)(want < most ? want : most);
     if (p.splits > kMostSplits) p.splits = kMostSplits;
     if (p.splits < 1) p.splits = 1;

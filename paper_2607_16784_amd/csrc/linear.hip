@@ -706,10 +706,11 @@ Plan plan_of(int32_t rows, int32_t n, int32_t k, int act)
         blocks = (tiles + (act == RM_ACT_SWIGLU ? 7 : 15)) / (act == RM_ACT_SWIGLU ? 8 : 16) *
                  ((rows + 63) / 64);
     }
-    // Parts of the columns until the CUs have about a workgroup each, of 1024 columns
-    // at least.  224 workgroups in one part and in two: 16 x 28672 x 4096 gated 22.1
-    // and 24.1 us, 32 rows 30.0 and 37.4, 64 rows 45.7 and 59.2.
-    const int64_t want = (kComputeUnits + blocks / 2) / blocks, most = k / 1024;
+    // Parts of the columns until the CUs have about a workgroup each, of 512 columns
+    // at least (64 x 512 x 8192: 17.6 us, of 1024 at least 19.5).  224 workgroups in
+    // one part and in two: 16 x 28672 x 4096 gated 22.1 and 24.1 us, 32 rows 30.0 and
+    // 37.4, 64 rows 45.7 and 59.2.
+    const int64_t want = (kComputeUnits + blocks / 2) / blocks, most = k / 512;
     p.parts_z = (int)(want < most ? want : most);
     // 64 x 2048 x 28672: 34.6 us in sixteen parts, 51.2 in eight
     if (p.parts_z > 16) p.parts_z = 16;
