@@ -313,9 +313,15 @@ __global__ __launch_bounds__(1024) void append_kernel(AppendArgs a, int32_t q_bl
     // value / scale = value * num / den: with den the largest magnitude itself a
     // quotient halfway between two codes comes out halfway
     const bool raised = !(now == was);
-    const float num = raised ? Q : 1.0f, den = raised ? top : was;
+    float num = raised ? Q : 1.0f, den = raised ? top : was;
     // magnitudes below 1e-36, whose reciprocal times Q is no number, count as 0
-    const float inv = den > 0.0f && Q / den < INFINITY ? 1.0f / den : 0.0f;
+    const bool known = den > 0.0f && Q / den < INFINITY;
+    // both times the power of two that brings den to [1/2, 1): a value times Q
+    // itself passes fp32 from 3.4e38 / Q on, and its quotient would be no number
+    const int power = known ? __builtin_amdgcn_frexp_expf(den) : 0;
+    num = ldexpf(num, -power);
+    den = ldexpf(den, -power);
+    const float inv = known ? 1.0f / den : 0.0f;
     if (t == 0) scales[block] = now;                // all have read the old one
     if (!in) return;
     uint8_t* codes = static_cast<uint8_t*>(value ? a.cache.v : a.cache.k) + block * TK * D;
