@@ -549,9 +549,10 @@ int rm_w4_linear(int32_t type, int32_t rows, int32_t n, int32_t k, const void* x
  * A page and head that gets new tokens: scale = max(scale of its older tokens,
  * largest new magnitude / Q), Q = 127 or 448; older codes become
  * round(code * old scale / scale), new ones round(value / scale) (ties to
- * even), and the slots behind the last token 0.  Where no new magnitude passes
- * 1e-36 the new codes may be 0.  A non-finite value makes the page's scale, and
- * so all that the head reads from the page, not finite.
+ * even), and the slots behind the last token 0.  The scale is rounded to fp32
+ * and the codes count in what is stored, subnormal scales too; below 2^-150 it
+ * is 0, and so are the codes.  A non-finite value makes the page's scale, and so
+ * all that the head reads from the page, not finite.
  * No page may be in two of the call's sequences where tokens are appended.
  * heads may be 0 (q and q_out are then not read).
  * Errors: RM_EINVAL (NULL pointer, negative size, rot odd or > head_dim, bad

@@ -310,23 +310,25 @@ __global__ __launch_bounds__(1024) void append_kernel(AppendArgs a, int32_t q_bl
     }
     if (!mine) return;
     const float now = MaxNan::of(was, top / Q);
-    // value / scale = value * num / den: with den the largest magnitude itself a
-    // quotient halfway between two codes comes out halfway
     const bool raised = !(now == was);
-    float num = raised ? Q : 1.0f, den = raised ? top : was;
-    // magnitudes below 1e-36, whose reciprocal times Q is no number, count as 0
-    const bool known = den > 0.0f && Q / den < INFINITY;
-    // both times the power of two that brings den to [1/2, 1): a value times Q
-    // itself passes fp32 from 3.4e38 / Q on, and its quotient would be no number
-    const int power = known ? __builtin_amdgcn_frexp_expf(den) : 0;
+    // value / scale = value * num / den.  With den the largest magnitude itself a
+    // quotient halfway between two codes comes out halfway; a scale in fp32's
+    // subnormal range is not that magnitude / Q to the last place, so there the
+    // codes count in the scale as it is stored
+    const bool by_top = raised && now >= 0x1p-126f;
+    float num = by_top ? Q : 1.0f, den = by_top ? top : now;
+    // both times the power of two that brings den to [1/2, 1), or near it where den
+    // is subnormal: a value times Q itself passes fp32 from 3.4e38 / Q on, and the
+    // reciprocal of a small den would be no number
+    const int power = max(__builtin_amdgcn_frexp_expf(den), -120);
     num = ldexpf(num, -power);
     den = ldexpf(den, -power);
-    const float inv = known ? 1.0f / den : 0.0f;
+    const float inv = den > 0.0f ? 1.0f / den : 0.0f;
     if (t == 0) scales[block] = now;                // all have read the old one
     if (!in) return;
     uint8_t* codes = static_cast<uint8_t*>(value ? a.cache.v : a.cache.k) + block * TK * D;
     const bool rescale = older > 0 && raised;
-    const float ratio = was * (num * inv);
+    const float ratio = rescale ? was / now : 0.0f;
     // what is written: the new tokens and zeros behind them, and with a raised
     // scale the older ones too
     const int lo = rescale ? 0 : older;
