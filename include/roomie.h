@@ -584,8 +584,8 @@ int rm_cache_read(int32_t type, const rm_cache* cache, int32_t n, const int32_t*
  * that sees nothing (its sequence or a page is out of range) gets 0.
  * q as in rm_rotary_append, out [n_tokens][heads][head_dim].  Logits, softmax
  * statistics and sums are fp32; a cached code is exact in the product's type;
- * the softmax weights enter the second product as f16 times the scale of the
- * values' page, relative to the largest such scale so far.
+ * the softmax weights enter the second product as f16 numbers, times the scale
+ * of the values' page and relative to the row's largest such product so far.
  * Tokens that a row does not see do not reach it, whatever their codes and
  * scales hold, with one exception: a value code that is e4m3's NaN (the append
  * writes none) reaches all of a call's own tokens of that sequence and head.

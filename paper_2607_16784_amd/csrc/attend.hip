@@ -13,7 +13,9 @@
 // operand is one 16-byte load.  Nothing passes through LDS until the waves join.
 //
 // Codes are exact in bf16 and f16.  Scales are constant over a page, so they
-// multiply the logits and, relative to the largest so far, the weights.
+// multiply the logits and the weights: what enters the second product is weight
+// times scale, relative to the row's own largest such product so far, which is
+// kept beside the maximum of its logits.
 //
 // A step of decoding is bound by reading the codes once.  The token axis is
 // split over the workgroup's waves and, when there are few tiles, over
@@ -28,7 +30,8 @@ constexpr int kBlock = 64;    // cached tokens a wave takes at a time
 constexpr int kWaves = 4;
 constexpr int kMostSplits = 256;
 // Weights and their sums carry 2^kLift, which the quotient takes off again: f16
-// holds weights in full down to 2^-28 of the largest, below that to 2^-39.
+// holds a weight times its page's scale in full down to 2^-28 of the row's largest,
+// below that to 2^-39.
 constexpr float kLift = 14.0f;
 
 __device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c)
@@ -206,7 +209,7 @@ attend_kernel(AttendArgs a, Plan plan)
     V q[C][D / 32];
     int32_t pos[C];
     f32x4 o[D / 16][C];
-    float m[C], l[C], ref = 0.0f;              // ref: largest scale of values so far
+    float m[C], l[C], ref[C];     // ref: largest e^(logit - m) * scale of values so far
     Pages now, next;
     int block = from + wave;
     if (block < upto) {
@@ -226,7 +229,7 @@ attend_kernel(AttendArgs a, Plan plan)
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         m[c] = -INFINITY;
-        l[c] = 0.0f;
+        l[c] = ref[c] = 0.0f;
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) o[d][c] = f32x4{0, 0, 0, 0};
     }
@@ -265,7 +268,11 @@ attend_kernel(AttendArgs a, Plan plan)
         const Pages after = ids(min(following + W, upto - 1));
         __builtin_amdgcn_sched_barrier(0);
         const bool whole = t0 >= t.all_lo && t0 + kBlock <= t.all_hi && !__any(bad);
-        float top[C];
+        // a scale that is not finite goes into the weights as it is and reaches
+        // the rows that see the page, not what their other weights are relative to
+        const float v_scale = near && !bad ? vs : 0.0f;
+        const float finite = fabsf(v_scale) < INFINITY ? fabsf(v_scale) : 0.0f;
+        float top[C], share[C], largest[C];
         bool moved = false;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
@@ -285,25 +292,27 @@ attend_kernel(AttendArgs a, Plan plan)
                     x = fmaxf(x, v);
                 }
             top[c] = fmaxf(m[c], rows_reduce<Max>(x));
-            moved |= top[c] > m[c];
+            // the lane's largest product of weight and scale; none where it sees nothing
+            const float base = top[c] == -INFINITY ? 0.0f : top[c];
+            const float here = rows_reduce<Max>(exp2_of(x - base) * finite);
+            const float kept = m[c] == -INFINITY ? 0.0f : ref[c] * exp2_of(m[c] - base);
+            largest[c] = fmaxf(kept, here);
+            moved |= top[c] > m[c] || here > kept;
         }
-        // a scale that is not finite goes into the weights as it is and reaches
-        // the rows that see the page, not the common factor
-        const float v_scale = near && !bad ? vs : 0.0f;
-        const float largest = fmaxf(ref, rows_reduce<Max>(v_scale < INFINITY ? v_scale : 0.0f));
-        if (__any(moved || largest > ref)) {
-            const float shrink = largest > 0.0f ? ref / largest : 1.0f;
+        if (__any(moved)) {
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const float f = top[c] == -INFINITY ? 1.0f : exp2_of(m[c] - top[c]);
                 l[c] *= f;
                 m[c] = top[c];
+                const float shrink = largest[c] > 0.0f ? ref[c] * f / largest[c] : 1.0f;
+                ref[c] = largest[c];
 #pragma unroll
-                for (int d = 0; d < D / 16; ++d) o[d][c] *= f * shrink;
+                for (int d = 0; d < D / 16; ++d) o[d][c] *= shrink;
             }
-            ref = largest;
         }
-        const float share = v_scale / (ref > 0.0f ? ref : 1.0f);
+#pragma unroll
+        for (int c = 0; c < C; ++c) share[c] = v_scale / (ref[c] > 0.0f ? ref[c] : 1.0f);
         f16x8 p[2][C];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
@@ -314,7 +323,7 @@ attend_kernel(AttendArgs a, Plan plan)
                 for (int k = 0; k < 4; ++k) {
                     const float e = exp2_of(sc[i][c][k] - base);
                     l[c] += e;
-                    float w = e * share;
+                    float w = e * share[c];
                     if (!whole) w = e == 0.0f ? 0.0f : w;
                     p[i >> 1][c][(i & 1) * 4 + k] = (f16)w;
                 }
@@ -359,7 +368,7 @@ attend_kernel(AttendArgs a, Plan plan)
     for (int c = 0; c < C; ++c) {
         float top = join_m[0][c * 16 + li];
         for (int w = 1; w < W; ++w) top = fmaxf(top, join_m[w][c * 16 + li]);
-        const float f = exp2_of(m[c] - (top == -INFINITY ? 0.0f : top)) * ref;
+        const float f = exp2_of(m[c] - (top == -INFINITY ? 0.0f : top)) * ref[c];
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) o[d][c] *= f;
     }
