@@ -363,12 +363,22 @@ attend_kernel(AttendArgs a, Plan plan)
         if (quad == 0) join_m[wave][c * 16 + li] = m[c], join_l[wave][c * 16 + li] = l[c];
     }
     __syncthreads();
+    // a row's maximum and sum over the waves
+    auto statistics = [&](int row, float& top, float& sum) {
+        top = join_m[0][row];
+        for (int w = 1; w < W; ++w) top = fmaxf(top, join_m[w][row]);
+        const float base = top == -INFINITY ? 0.0f : top;
+        sum = 0.0f;
+        for (int w = 0; w < W; ++w) sum += join_l[w][row] * exp2_of(join_m[w][row] - base);
+    };
     // [wave][d / 4][row][4]: neighbouring lanes write neighbouring rows
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        float top = join_m[0][c * 16 + li];
-        for (int w = 1; w < W; ++w) top = fmaxf(top, join_m[w][c * 16 + li]);
-        const float f = exp2_of(m[c] - (top == -INFINITY ? 0.0f : top)) * ref[c];
+        float top, sum;
+        statistics(c * 16 + li, top, sum);
+        // the wave's share of the mean, so that no sum passes the largest value
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        const float f = exp2_of(m[c] - (top == -INFINITY ? 0.0f : top)) * inv * ref[c];
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) o[d][c] *= f;
     }
@@ -402,17 +412,11 @@ attend_kernel(AttendArgs a, Plan plan)
     const int64_t n_parts = (int64_t)gridDim.x;
     for (int u = threadIdx.x; u < t.rows * (D / 8); u += W * 64) {
         const int row = u / (D / 8), d = u % (D / 8) * 8;
-        float top = join_m[0][row];
-        for (int w = 1; w < W; ++w) top = fmaxf(top, join_m[w][row]);
-        const float base = top == -INFINITY ? 0.0f : top;
-        float sum = 0.0f;
-        for (int w = 0; w < W; ++w) sum += join_l[w][row] * exp2_of(join_m[w][row] - base);
         const f32x4 v0 = sums[(d / 4) * H + row], v1 = sums[(d / 4 + 1) * H + row];
         if (plan.splits == 1) {
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
             V r;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) r[i] = (T)(v0[i] * inv), r[4 + i] = (T)(v1[i] * inv);
+            for (int i = 0; i < 4; ++i) r[i] = (T)v0[i], r[4 + i] = (T)v1[i];
             const int rr = tile * H + row;
             store8(static_cast<T*>(a.out) +
                        ((int64_t)(s.first + rr / G) * a.heads + head * G + rr % G) * D + d, r);
@@ -422,14 +426,13 @@ attend_kernel(AttendArgs a, Plan plan)
             reinterpret_cast<f32x4*>(to)[1] = v1;
             if (d == 0) {
                 float* ml = part + n_parts * H * D + ((int64_t)blockIdx.x * H + row) * 2;
-                ml[0] = top;
-                ml[1] = sum;
+                statistics(row, ml[0], ml[1]);
             }
         }
     }
 }
 
-// A workgroup a row of a tile: the splits' partial results.  A wave takes every
+// A workgroup a row of a tile: the splits' means, weighted.  A wave takes every
 // fourth split, a lane the splits' maxima and sums first.
 template <typename T, int D, int C>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, Plan plan, int64_t n_parts)
@@ -460,10 +463,11 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, Plan pla
     for (int i = lane; i < plan.splits; i += 64) {
         const float f = exp2_of(ml[(int64_t)i * H * 2] - base), l = ml[(int64_t)i * H * 2 + 1];
         sum = __builtin_fmaf(l, f, sum);
-        // a split that saw nothing may not have written its sums
-        if (wave == 0) factor[i] = l == 0.0f ? -1.0f : f;
+        // a split that saw nothing may not have written its mean
+        if (wave == 0) factor[i] = l == 0.0f ? -1.0f : f * l;
     }
     sum = wave_reduce<Add>(sum);
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     __syncthreads();
     float v[N];
 #pragma unroll
@@ -472,21 +476,20 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, Plan pla
     typedef float Vn __attribute__((ext_vector_type(N)));
 #pragma unroll 4
     for (int i = wave; i < plan.splits; i += 4) {
-        const float f = factor[i];
+        const float weight = factor[i], f = weight * inv;
         const Vn x = *reinterpret_cast<const Vn*>(from + (int64_t)i * H * D);
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            v[k] = f < 0.0f ? v[k] : __builtin_fmaf(x[k], f, v[k]);
+            v[k] = weight < 0.0f ? v[k] : __builtin_fmaf(x[k], f, v[k]);
         }
     }
 #pragma unroll
     for (int k = 0; k < N; ++k) sums[wave][lane * N + k] = v[k];
     __syncthreads();
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     T* out = static_cast<T*>(a.out) +
              ((int64_t)(s.first + rr / G) * a.heads + head * G + rr % G) * D;
     for (int d = threadIdx.x; d < D; d += 256)
-        out[d] = (T)((sums[0][d] + sums[1][d] + sums[2][d] + sums[3][d]) * inv);
+        out[d] = (T)(sums[0][d] + sums[1][d] + sums[2][d] + sums[3][d]);
 }
 
 // 64 rows a tile need all registers of a SIMD for one wave: chunks of prompts
