@@ -32,7 +32,7 @@ constexpr int kMostSplits = 256;
 // Weights and their sums carry 2^kLift, which the quotient takes off again: f16
 // holds a weight times its page's scale in full down to 2^-28 of the row's largest,
 // below that to 2^-39.
-constexpr float kLift = 14.0f;
+constexpr float kLift = 15.0f;
 
 __device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c)
 {
@@ -209,7 +209,9 @@ attend_kernel(AttendArgs a, Plan plan)
     V q[C][D / 32];
     int32_t pos[C];
     f32x4 o[D / 16][C];
-    float m[C], l[C], ref[C];     // ref: largest e^(logit - m) * scale of values so far
+    // m and r: the largest logit so far, alone and times the scale of its values,
+    // both as powers of two
+    float m[C], l[C], r[C];
     Pages now, next;
     int block = from + wave;
     if (block < upto) {
@@ -229,7 +231,8 @@ attend_kernel(AttendArgs a, Plan plan)
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         m[c] = -INFINITY;
-        l[c] = ref[c] = 0.0f;
+        r[c] = -INFINITY;
+        l[c] = 0.0f;
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) o[d][c] = f32x4{0, 0, 0, 0};
     }
@@ -268,11 +271,14 @@ attend_kernel(AttendArgs a, Plan plan)
         const Pages after = ids(min(following + W, upto - 1));
         __builtin_amdgcn_sched_barrier(0);
         const bool whole = t0 >= t.all_lo && t0 + kBlock <= t.all_hi && !__any(bad);
-        // a scale that is not finite goes into the weights as it is and reaches
-        // the rows that see the page, not what their other weights are relative to
+        // scale = part * 2^power; one that is not finite goes into the weights as it
+        // is and reaches the rows that see the page, not what their others are
+        // relative to
         const float v_scale = near && !bad ? vs : 0.0f;
-        const float finite = fabsf(v_scale) < INFINITY ? fabsf(v_scale) : 0.0f;
-        float top[C], share[C], largest[C];
+        const bool finite = fabsf(v_scale) < INFINITY;
+        const float power = finite && v_scale != 0.0f
+                                ? (float)__builtin_amdgcn_frexp_expf(v_scale) : -INFINITY;
+        float top[C], share[C], high[C];
         bool moved = false;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
@@ -292,27 +298,26 @@ attend_kernel(AttendArgs a, Plan plan)
                     x = fmaxf(x, v);
                 }
             top[c] = fmaxf(m[c], rows_reduce<Max>(x));
-            // the lane's largest product of weight and scale; none where it sees nothing
-            const float base = top[c] == -INFINITY ? 0.0f : top[c];
-            const float here = rows_reduce<Max>(exp2_of(x - base) * finite);
-            const float kept = m[c] == -INFINITY ? 0.0f : ref[c] * exp2_of(m[c] - base);
-            largest[c] = fmaxf(kept, here);
-            moved |= top[c] > m[c] || here > kept;
+            high[c] = fmaxf(r[c], rows_reduce<Max>(x + power));
+            moved |= top[c] > m[c] || high[c] > r[c];
         }
         if (__any(moved)) {
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                const float f = top[c] == -INFINITY ? 1.0f : exp2_of(m[c] - top[c]);
-                l[c] *= f;
+                l[c] *= top[c] == -INFINITY ? 1.0f : exp2_of(m[c] - top[c]);
+                const float shrink = high[c] == -INFINITY ? 1.0f : exp2_of(r[c] - high[c]);
                 m[c] = top[c];
-                const float shrink = largest[c] > 0.0f ? ref[c] * f / largest[c] : 1.0f;
-                ref[c] = largest[c];
+                r[c] = high[c];
 #pragma unroll
                 for (int d = 0; d < D / 16; ++d) o[d][c] *= shrink;
             }
         }
+        // the exponent is bounded where the weights beside it are 0
 #pragma unroll
-        for (int c = 0; c < C; ++c) share[c] = v_scale / (ref[c] > 0.0f ? ref[c] : 1.0f);
+        for (int c = 0; c < C; ++c)
+            share[c] = finite ? __builtin_amdgcn_frexp_mantf(v_scale) *
+                                    exp2_of(fminf(m[c] - r[c] + power, 126.0f))
+                              : v_scale;
         f16x8 p[2][C];
 #pragma unroll
         for (int c = 0; c < C; ++c) {
@@ -378,7 +383,8 @@ attend_kernel(AttendArgs a, Plan plan)
         statistics(c * 16 + li, top, sum);
         // the wave's share of the mean, so that no sum passes the largest value
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        const float f = exp2_of(m[c] - (top == -INFINITY ? 0.0f : top)) * inv * ref[c];
+        const float f = exp2_of(r[c] - (top == -INFINITY ? 0.0f : top) - kLift) *
+                        (inv * (float)(1 << (int)kLift));
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) o[d][c] *= f;
     }
