@@ -506,7 +506,9 @@ typedef struct {
     int32_t table_stride;          /* pages that a row of the table can name   */
     int32_t n_tokens;              /* rows of the token arrays                 */
     int32_t max_tokens;            /* bound on n_b (host); a sequence with more
-                                      sets RM_ST_BAD_LENGTH and is skipped     */
+                                      sets RM_ST_BAD_LENGTH and is skipped.
+                                      A row is in one sequence at most; rows
+                                      in none are padding                      */
 } rm_sequences;
 
 /*
@@ -581,7 +583,8 @@ int rm_cache_read(int32_t type, const rm_cache* cache, int32_t n, const int32_t*
  *   out[t][h] = sum_j w_j value_j,  w = softmax over j of scale * q[t][h].key_j
  * of kv head h / (heads / kv_heads), over the tokens j of t's sequence that it
  * sees: j <= p, its own index, and, where window > 0, j > p - window.  A token
- * that sees nothing (its sequence or a page is out of range) gets 0.
+ * that sees nothing (its sequence or a page is out of range) gets 0, and so do
+ * rows that no sequence holds.
  * q as in rm_rotary_append, out [n_tokens][heads][head_dim].  Logits, softmax
  * statistics and sums are fp32; a cached code is exact in the product's type;
  * the softmax weights enter the second product as f16 numbers, times the scale

@@ -95,6 +95,9 @@ __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 struct Plan {
     int32_t tiles, splits;      // tiles of rows a sequence and kv head; splits of a tile
     int32_t rows;               // of a tile that a sequence can have
+    int32_t columns;            // a tile has 16 times as many rows
+    int32_t clear;              // workgroups behind the tiles', for clear_rows
+    int64_t parts;              // splits of all tiles
 };
 
 // Rows and token range of a tile.
@@ -117,6 +120,41 @@ __device__ inline Tile tile_of(const Sequence& s, int32_t group, int32_t window,
     return t;
 }
 
+// Zeros for those of the rows from kClear * group on that no sequence holds, or one
+// that is out of range.  The sequences need not be in order, so all of them are
+// asked; the rows that they hold are marked in LDS.
+constexpr int kClear = 512;
+
+template <typename T, int D>
+__device__ inline void clear_rows(const AttendArgs& a, int group)
+{
+    __shared__ uint32_t held[kClear / 32];
+    const int64_t r0 = (int64_t)group * kClear;
+    const int count = (int)min((int64_t)kClear, a.seqs.n_tokens - r0);
+    if (threadIdx.x < kClear / 32) held[threadIdx.x] = 0;
+    __syncthreads();
+    for (int b = threadIdx.x; b < a.seqs.n_seqs; b += kWaves * 64) {
+        const Sequence s = sequence_of(a.seqs, a.cache.page_tokens, b);
+        const int64_t lo = max((int64_t)s.first, r0) - r0;
+        const int64_t hi = min((int64_t)s.first + s.n, r0 + count) - r0;
+        for (int64_t r = lo; r < hi; r = (r / 32 + 1) * 32) {
+            const int n = (int)min((int64_t)32, hi - r / 32 * 32);
+            atomicOr(&held[r / 32], (n == 32 ? ~0u : (1u << n) - 1) & ~0u << (r % 32));
+        }
+    }
+    __syncthreads();
+    const int64_t row = (int64_t)a.heads * D;
+    for (int w = 0; w < (count + 31) / 32; ++w) {
+        uint32_t none = ~(uint32_t)__builtin_amdgcn_readfirstlane(held[w]);
+        for (; none; none &= none - 1) {
+            const int r = w * 32 + __ffs(none) - 1;
+            if (r >= count) break;
+            for (int64_t i = threadIdx.x * 8; i < row; i += kWaves * 64 * 8)
+                store8(static_cast<T*>(a.out) + (r0 + r) * row + i, typename Vec<T>::x8{});
+        }
+    }
+}
+
 // Two waves a SIMD where the registers allow it: left to itself the compiler
 // takes all registers for one (32 rows, chunks of prompts: 209 us, with two 134).
 template <typename T, int FMT, int D, int C>
@@ -130,7 +168,12 @@ attend_kernel(AttendArgs a, Plan plan)
     __shared__ float join_m[W][H], join_l[W][H];
 
     const int KV = a.cache.kv_heads, TK = a.cache.page_tokens, G = a.heads / KV;
-    int64_t at = blockIdx.x;
+    const int64_t part_at = blockIdx.x;
+    if (part_at >= plan.parts) {
+        clear_rows<T, D>(a, (int)(part_at - plan.parts));
+        return;
+    }
+    int64_t at = part_at;
     const int split = (int)(at % plan.splits);
     at /= plan.splits;
     const int tile = (int)(at % plan.tiles);
@@ -141,15 +184,11 @@ attend_kernel(AttendArgs a, Plan plan)
     const int li = lane & 15, quad = lane >> 4;
 
     if (s.n == 0) {
-        // no token, or one of a sequence that is out of range: zeros
         if (s.bad && a.status && threadIdx.x == 0) atomicOr(a.status, RM_ST_BAD_LENGTH);
-        if (tile || split) return;
-        int64_t from = b, upto = (int64_t)b + 1;
-        if (a.seqs.token_offsets) from = s.first, upto = a.seqs.token_offsets[b + 1];
-        if (from < 0 || upto > a.seqs.n_tokens) return;
-        for (int64_t t = from; t < upto; ++t)
-            for (int i = threadIdx.x; i < G * D; i += W * 64)
-                static_cast<T*>(a.out)[(t * a.heads + head * G) * D + i] = (T)0.0f;
+        // with token_offsets the rows are cleared by clear_rows
+        if (a.seqs.token_offsets || tile || split) return;
+        for (int i = threadIdx.x; i < G * D; i += W * 64)
+            static_cast<T*>(a.out)[((int64_t)b * a.heads + head * G) * D + i] = (T)0.0f;
         return;
     }
     if (tile * H >= s.n * G) return;
@@ -415,7 +454,6 @@ attend_kernel(AttendArgs a, Plan plan)
     }
     __syncthreads();
     float* part = static_cast<float*>(a.workspace);
-    const int64_t n_parts = (int64_t)gridDim.x;
     for (int u = threadIdx.x; u < t.rows * (D / 8); u += W * 64) {
         const int row = u / (D / 8), d = u % (D / 8) * 8;
         const f32x4 v0 = sums[(d / 4) * H + row], v1 = sums[(d / 4 + 1) * H + row];
@@ -427,11 +465,11 @@ attend_kernel(AttendArgs a, Plan plan)
             store8(static_cast<T*>(a.out) +
                        ((int64_t)(s.first + rr / G) * a.heads + head * G + rr % G) * D + d, r);
         } else {
-            float* to = part + ((int64_t)blockIdx.x * H + row) * D + d;
+            float* to = part + (part_at * H + row) * D + d;
             reinterpret_cast<f32x4*>(to)[0] = v0;
             reinterpret_cast<f32x4*>(to)[1] = v1;
             if (d == 0) {
-                float* ml = part + n_parts * H * D + ((int64_t)blockIdx.x * H + row) * 2;
+                float* ml = part + plan.parts * H * D + (part_at * H + row) * 2;
                 statistics(row, ml[0], ml[1]);
             }
         }
@@ -441,7 +479,7 @@ attend_kernel(AttendArgs a, Plan plan)
 // A workgroup a row of a tile: the splits' means, weighted.  A wave takes every
 // fourth split, a lane the splits' maxima and sums first.
 template <typename T, int D, int C>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, Plan plan, int64_t n_parts)
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, Plan plan)
 {
     constexpr int H = 16 * C, N = D / 64;
     __shared__ float factor[kMostSplits];
@@ -459,7 +497,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, Plan pla
     const int rr = tile * H + row;
     if (rr >= s.n * G) return;
     const float* part = static_cast<const float*>(a.workspace);
-    const float* ml = part + n_parts * H * D + (block * H + row) * 2;
+    const float* ml = part + plan.parts * H * D + (block * H + row) * 2;
     // every wave the same: one split a lane, then the next 64
     float top = -INFINITY;
     for (int i = lane; i < plan.splits; i += 64) top = fmaxf(top, ml[(int64_t)i * H * 2]);
@@ -507,9 +545,12 @@ int columns_of(int64_t rows)
 
 Plan plan_of(const rm_cache& c, const rm_sequences& s, int32_t heads)
 {
-    const int64_t rows = (int64_t)s.max_tokens * (heads / c.kv_heads);
-    const int height = 16 * columns_of(rows);
+    // a tile a sequence at least: it reports one that is out of range
+    const int64_t rows = (int64_t)(s.max_tokens > 1 ? s.max_tokens : 1) * (heads / c.kv_heads);
     Plan p;
+    p.columns = columns_of(rows);
+    const int height = 16 * p.columns;
+    p.clear = s.token_offsets ? (int32_t)(((int64_t)s.n_tokens + kClear - 1) / kClear) : 0;
     p.tiles = (int32_t)((rows + height - 1) / height);
     p.rows = (int32_t)(rows < height ? rows : height);
     const int64_t units = (int64_t)s.n_seqs * c.kv_heads * p.tiles;
@@ -525,16 +566,16 @@ Plan plan_of(const rm_cache& c, const rm_sequences& s, int32_t heads)
     p.splits = (int32_t)(want < most ? want : most);
     if (p.splits > kMostSplits) p.splits = kMostSplits;
     if (p.splits < 1) p.splits = 1;
+    p.parts = units * p.splits;
     return p;
 }
 
 template <typename T, int FMT, int D, int C>
 hipError_t launch_columns(const AttendArgs& a, const Plan& p, hipStream_t s)
 {
-    const int64_t units = (int64_t)a.seqs.n_seqs * a.cache.kv_heads * p.tiles;
-    const int64_t parts = units * p.splits;
-    if (parts == 0) return hipSuccess;
-    if (parts > 0x7fffffff || units * p.rows > 0x7fffffff) return hipErrorInvalidValue;
+    const int64_t blocks = p.parts + p.clear, rows = p.parts / p.splits * p.rows;
+    if (blocks == 0) return hipSuccess;
+    if (blocks > 0x7fffffff || rows > 0x7fffffff) return hipErrorInvalidValue;
     const size_t lds = (size_t)(kWaves / 2) * 16 * C * D * sizeof(float);    // 64 KB at most
     const auto kernel = attend_kernel<T, FMT, D, C>;
     if (lds > 60 * 1024) {      // with the static arrays over 64 KB
@@ -543,17 +584,16 @@ hipError_t launch_columns(const AttendArgs& a, const Plan& p, hipStream_t s)
                                                  (int)lds);
         if (e != hipSuccess) return e;
     }
-    hipError_t e = launch(kernel, dim3((unsigned)parts), kWaves * 64, lds, s, a, p);
-    if (e != hipSuccess || p.splits == 1) return e;
-    return launch(attend_join_kernel<T, D, C>, dim3((unsigned)(units * p.rows)), 256, 0, s, a, p,
-                  parts);
+    hipError_t e = launch(kernel, dim3((unsigned)blocks), kWaves * 64, lds, s, a, p);
+    if (e != hipSuccess || p.splits == 1 || rows == 0) return e;
+    return launch(attend_join_kernel<T, D, C>, dim3((unsigned)rows), 256, 0, s, a, p);
 }
 
 template <typename T, int FMT, int D>
 hipError_t launch_dim(const AttendArgs& a, hipStream_t s)
 {
     const Plan p = plan_of(a.cache, a.seqs, a.heads);
-    if (columns_of((int64_t)a.seqs.max_tokens * (a.heads / a.cache.kv_heads)) == 1)
+    if (p.columns == 1)
         return launch_columns<T, FMT, D, 1>(a, p, s);
     return launch_columns<T, FMT, D, 2>(a, p, s);
 }
@@ -572,9 +612,7 @@ size_t attend_workspace(const rm_cache& c, const rm_sequences& s, int32_t heads)
 {
     const Plan p = plan_of(c, s, heads);
     if (p.splits == 1) return 256;
-    const int height = 16 * columns_of((int64_t)s.max_tokens * (heads / c.kv_heads));
-    const size_t parts = (size_t)s.n_seqs * c.kv_heads * p.tiles * p.splits;
-    return (parts * height * (c.head_dim + 2) * sizeof(float) + 255) / 256 * 256;
+    return ((size_t)p.parts * 16 * p.columns * (c.head_dim + 2) * sizeof(float) + 255) / 256 * 256;
 }
 
 hipError_t launch_attend(int type, const AttendArgs& a, hipStream_t s)
