@@ -464,8 +464,9 @@ __global__ __launch_bounds__(256) void cache_read_kernel(rm_cache c, int32_t n,
 hipError_t launch_append(int type, const AppendArgs& a, hipStream_t s)
 {
     const int TK = a.cache.page_tokens;
-    const int32_t pages = a.seqs.max_tokens > 0
-                              ? (int32_t)(((int64_t)a.seqs.max_tokens + 2 * TK - 2) / TK) : 0;
+    // one a sequence at least: it reports one that is out of range
+    const int64_t most = a.seqs.max_tokens > 1 ? a.seqs.max_tokens : 1;
+    const int32_t pages = (int32_t)((most + 2 * TK - 2) / TK);
     const int tile = TK * a.cache.head_dim / 32;
     const int group = tile < 64 ? 64 : tile, threads = group < 256 ? 256 : group;
     const int groups = threads / group, waves = threads / 64;
