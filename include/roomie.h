@@ -521,7 +521,8 @@ typedef struct {
  *   half.  scales [n][ceil(k/group)]; zeros uint8 [n][ceil(k/group)], values
  *   0..15 (NULL: 8 everywhere); bias [n] or NULL.  y: rows of n (SWIGLU: n/2)
  *   elements, y_stride apart.  Sums are fp32, each output is rounded once.
- *   An infinity in x may give NaN.
+ *   An infinity in x may give NaN, and so may a bfloat16 scale of 2^123 (1e37)
+ *   or more; no other x and scales overflow before their result does.
  * Some sizes split the columns over workgroups and join the parts through the
  *   workspace, rm_w4_linear_workspace_bytes bytes, 256-byte aligned (0 bytes:
  *   none, workspace may be NULL).  The order of every sum is fixed.

@@ -7,11 +7,15 @@
 //
 // Expansion: two codes sit 4 nibbles apart in a word, so (w >> 4s) & 0x000f000f
 // is the pair (s, s+4) in the low bits of two 16-bit numbers, and OR-ing an
-// exponent makes it 128 + code (bf16) or 1024 + code (f16), exactly.  x is put
-// into the same order 0 4 1 5 2 6 3 7.  f16 then subtracts 1024 + zero (exact).
+// exponent makes it (128 + code) * 2^-15 (bf16) or 1024 + code (f16), exactly.  x is
+// put into the same order 0 4 1 5 2 6 3 7.  f16 then subtracts 1024 + zero (exact).
 // bf16 has no packed addition: the product is taken with 128 + code and
-// (128 + zero) * (sum of x) is subtracted from each group's fp32 sum.  Both keep
-// the code exact; the group's scale multiplies the fp32 sum.
+// (128 + zero) * (sum of x) is subtracted from each group's fp32 sum, so partial
+// sums are up to 143 times the terms: in fp32 still 2^8 finer than the output's
+// rounding.  The 2^-15 keeps the sum over a group of the largest bf16 numbers
+// finite; 2^5 of it come off with the group's scale, 2^10 with the bias, so that
+// neither end of fp32 costs a result that bf16 holds.  Both keep the code exact;
+// the group's scale multiplies the fp32 sum.
 //
 // What costs next to the codes is the number of vector memory accesses, not
 // their bytes: an operand's 16 rows are 64 accesses of 16 bytes an instruction,
@@ -102,6 +106,9 @@ __device__ inline float finish(float t, float other)
     return ACT == RM_ACT_SWIGLU ? t / (1.0f + expf(-t)) * other : t;
 }
 
+// Unit of the accumulators.
+template <typename T> constexpr float kUnit = __is_same(T, f16) ? 1.0f : 0x1p10f;
+
 constexpr int kStep = 128;    // columns of a step: 16 bytes of codes a lane
 
 // Shape of a workgroup.  RG waves side by side, each with 16 R rows of W, and
@@ -129,7 +136,7 @@ struct Tile {
     f32x4 acc[S::R][S::M];
     Expander expander;
 
-    __device__ Tile() : expander(S::HALF ? 0x64006400u : 0x43004300u)
+    __device__ Tile() : expander(S::HALF ? 0x64006400u : 0x3b803b80u)
     {
 #pragma unroll
         for (int r = 0; r < S::R; ++r)
@@ -137,7 +144,7 @@ struct Tile {
             for (int m = 0; m < S::M; ++m) acc[r][m] = f32x4{0, 0, 0, 0};
     }
 
-    // x_of(m, j) in the expanded order, sum_of(p, m); group_of(p, r): the
+    // x_of(m, j) in the expanded order, sum_of(p, m) in units of 2^7; group_of(p, r): the
     // scale's bits below, the zero above
     template <class X, class Sum, class Group>
     __device__ inline void step(X x_of, Sum sum_of, u32x4 (&w)[S::R], Group group_of)
@@ -178,7 +185,7 @@ struct Tile {
                 if (!S::HALF) sum = sum_of(p, m);
 #pragma unroll
                 for (int r = 0; r < S::R; ++r) {
-                    const float bias = -128.0f - z[r];
+                    const float bias = __builtin_fmaf(z[r], -0x1p-8f, -0.5f);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float q = S::HALF ? part[r][m][i]
@@ -223,7 +230,7 @@ struct Stage {
         if (!S::HALF) {
             float s = 0.0f;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) s += (float)v[k];
+            for (int k = 0; k < 8; ++k) s = __builtin_fmaf((float)v[k], 0x1p-7f, s);
             s += dpp_float<0xB1>(s);
             s += dpp_float<0x4E>(s);
             if (S::PER >= 2) s += dpp_float<0x141>(s);
@@ -274,7 +281,10 @@ template <class S>
 __device__ inline uint32_t group_word(const LinearArgs& a, int64_t row, int g)
 {
     const int groups = (a.k + a.group - 1) / a.group;
-    const uint32_t scale = static_cast<const uint16_t*>(a.scales)[row * groups + g];
+    typedef typename S::type T;
+    T s = static_cast<const T*>(a.scales)[row * groups + g];
+    if (!S::HALF) s = (T)((float)s * 32.0f);       // exact
+    const uint32_t scale = __builtin_bit_cast(uint16_t, s);
     return scale | (a.zeros ? (uint32_t)a.zeros[row * groups + g] : 8u) << 16;
 }
 
@@ -292,13 +302,13 @@ __device__ inline void rest(const LinearArgs& a, Tile<S>& tile, int rg, int m0, 
     for (int step = first; step < steps; step += by) {
         const int k0 = step * kStep;
         u32x4 w[S::R];
-        V x[S::M][4], ones;
+        V x[S::M][4], units;
 #pragma unroll
         for (int r = 0; r < S::R; ++r)
             w[r] = load_codes(a.codes + row_of<S>(a, (rg * S::R + r) * 16 + li) * a.code_stride,
                               k0 + quad * 32, row_bytes);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ones[i] = (T)1.0f;
+        for (int i = 0; i < 8; ++i) units[i] = (T)0x1p-7f;
 #pragma unroll
         for (int m = 0; m < S::M; ++m) {
             const T* row = static_cast<const T*>(a.x) +
@@ -314,7 +324,7 @@ __device__ inline void rest(const LinearArgs& a, Tile<S>& tile, int rg, int m0, 
                       f32x4 sum = {0, 0, 0, 0};
 #pragma unroll
                       for (int j = p * S::PER; j < (p + 1) * S::PER; ++j)
-                          sum = mfma(x[m][j], ones, sum);
+                          sum = mfma(x[m][j], units, sum);
                       return sum;
                   },
                   w,
@@ -379,7 +389,8 @@ __device__ inline void finish_tile(const LinearArgs& a, Tile<S>& tile, char* lds
             for (int i = 0; i < 4; ++i)
                 if (row + i < a.rows)
                     static_cast<T*>(a.y)[(row + i) * a.y_stride + j] = (T)finish<S::ACT>(
-                        tile.acc[r][m][i] + b0, tile.acc[(r + R - HR) % R][m][i] + b1);
+                        __builtin_fmaf(tile.acc[r][m][i], kUnit<T>, b0),
+                        __builtin_fmaf(tile.acc[(r + R - HR) % R][m][i], kUnit<T>, b1));
         }
     }
 }
@@ -621,7 +632,8 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs a, int32_t 
     for (int i = 0; i < 4; ++i)
         if (quad * 4 + i < a.rows)
             static_cast<T*>(a.y)[(quad * 4 + i) * a.y_stride + j] =
-                (T)finish<ACT>(sum[0][i] + b0, sum[1][i] + b1);
+                (T)finish<ACT>(__builtin_fmaf(sum[0][i], kUnit<T>, b0),
+                               __builtin_fmaf(sum[1][i], kUnit<T>, b1));
 }
 
 template <class S, typename K, typename... A>

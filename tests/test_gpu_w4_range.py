@@ -57,9 +57,13 @@ def test_large_inputs_behind_a_gate():
     scales[:40] *= 2.0 ** -120                   # gates of some 1
     got = api.rm_w4_linear(x, codes, scales.bfloat16(), 64, zeros=z, act="swiglu")
     want = ref.linear(x, codes, scales.bfloat16(), 64, z, None, "swiglu")
-    assert torch.all(torch.isfinite(got))
+    # bf16 ends at 3.39e38; a few products of gate and value are beyond
+    fits, beyond = want.abs() < 3.38e38, want.abs() > 3.41e38
+    assert int(beyond.sum()) == 5 and torch.all(fits | beyond)
+    got = ref.f64(got)
+    assert torch.all(torch.isfinite(got[fits])) and torch.all(got[beyond] == want[beyond] * float("inf"))
     # what 143 times the terms loses in fp32, of terms that partly cancel
-    assert float((ref.f64(got) - want).norm() / want.norm()) < 2.0 ** -8
+    assert float((got - want)[fits].norm() / want[fits].norm()) < 2.0 ** -8
 
 
 @pytest.mark.parametrize("size", SIZES, ids=["x".join(map(str, s)) for s in SIZES])
