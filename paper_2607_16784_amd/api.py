@@ -416,25 +416,25 @@ def rm_place_optimal(delay, iso_time, kernel_count, models, n_devices, capacity,
 # These run before every launch of a few microseconds, so they are written for
 # the accepted case: one expression, the message only where it fails.
 
-def _on_gpu(t, dtype, shape, name):
-    """Address of a contiguous GPU tensor of this type and shape; None for None."""
+def _on_gpu(t, dtype, shape, gpu, name):
+    """Address of a contiguous tensor of this type and shape on this GPU; None for None."""
     if t is None:
         return None
-    if t.is_cuda and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+    if t.get_device() == gpu and t.dtype is dtype and t.shape == shape and t.is_contiguous():
         return t.data_ptr()
-    raise ValueError(f"{name}: expected a contiguous GPU tensor of {dtype} and shape "
-                     f"{tuple(shape)}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    raise ValueError(f"{name}: expected a contiguous tensor of {dtype} and shape {tuple(shape)} "
+                     f"on cuda:{gpu}, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
-def _rows(t, dtype, shape, name):
-    """Strides of a GPU tensor whose last axis is consecutive."""
-    if t.is_cuda and t.dtype is dtype and t.shape == shape:
+def _rows(t, dtype, shape, gpu, name):
+    """Strides of a tensor on this GPU whose last axis is consecutive."""
+    if t.get_device() == gpu and t.dtype is dtype and t.shape == shape:
         strides = t.stride()
         if strides[-1] == 1 or shape[-1] <= 1:
             return strides
         raise ValueError(f"{name}: the last axis must be consecutive")
-    raise ValueError(f"{name}: expected a GPU tensor of {dtype} and shape {tuple(shape)}, "
-                     f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    raise ValueError(f"{name}: expected a tensor of {dtype} and shape {tuple(shape)} on "
+                     f"cuda:{gpu}, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 def _pitch(stride, rows, width, name):
@@ -447,11 +447,12 @@ def _pitch(stride, rows, width, name):
 
 
 def _type_of(t, name):
-    code = TYPES.get(t.dtype)
-    if code is None or not t.is_cuda:
+    """The type's code and the GPU that all tensors of the call have to be on."""
+    code, gpu = TYPES.get(t.dtype), t.get_device()
+    if code is None or gpu < 0:
         raise ValueError(f"{name}: expected a GPU tensor of bfloat16 or float16, got {t.dtype} "
                          f"on {t.device}")
-    return code
+    return code, gpu
 
 
 def _named(names, value, what):
@@ -462,6 +463,16 @@ def _named(names, value, what):
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_gpu = getattr(torch._C, "_cuda_getDevice", None)
+
+
+def _call(function, gpu, *args):
+    """The entry point on this GPU and its current stream.  The GPU has to be the
+    current one: a default stream's handle is 0 on every GPU."""
+    if _current_gpu() == gpu:
+        return function(*args, _raw_stream(gpu))
+    with torch.cuda.device(gpu):
+        return function(*args, _raw_stream(gpu))
 
 
 def new_cache(n_pages, kv_heads, page_tokens, head_dim, codes=torch.int8, device="cuda"):
@@ -478,27 +489,27 @@ def new_cache(n_pages, kv_heads, page_tokens, head_dim, codes=torch.int8, device
             "v_scale": torch.zeros(shape, dtype=torch.float32, device=device)}
 
 
-def _cache_of(cache):
+def _cache_of(cache, gpu):
     k, v, ks, vs = cache["k"], cache["v"], cache["k_scale"], cache["v_scale"]
     codes = CODES.get(k.dtype)
     if k.dim() != 4 or codes is None:
         raise ValueError("cache: expected codes int8 or float8_e4m3fn [pages, kv_heads, "
                          f"page_tokens, head_dim], got {k.dtype} {tuple(k.shape)}")
     shape = pages, heads, tokens, dim = k.shape
-    return Cache(_on_gpu(k, k.dtype, shape, "cache k"),
-                 _on_gpu(v, k.dtype, (pages, heads, dim, tokens), "cache v"),
-                 _on_gpu(ks, torch.float32, (pages, heads), "cache k_scale"),
-                 _on_gpu(vs, torch.float32, (pages, heads), "cache v_scale"),
+    return Cache(_on_gpu(k, k.dtype, shape, gpu, "cache k"),
+                 _on_gpu(v, k.dtype, (pages, heads, dim, tokens), gpu, "cache v"),
+                 _on_gpu(ks, torch.float32, (pages, heads), gpu, "cache k_scale"),
+                 _on_gpu(vs, torch.float32, (pages, heads), gpu, "cache v_scale"),
                  pages, heads, tokens, dim, codes)
 
 
-def _sequences_of(table, lengths, token_offsets, n_tokens, max_tokens):
+def _sequences_of(table, lengths, token_offsets, n_tokens, max_tokens, gpu):
     if table.dim() != 2:
         raise ValueError("table: expected [sequences, pages]")
     n, pages = shape = table.shape
-    return Sequences(_on_gpu(table, torch.int32, shape, "table"),
-                     _on_gpu(lengths, torch.int32, (n,), "lengths"),
-                     _on_gpu(token_offsets, torch.int32, (n + 1,), "token_offsets"),
+    return Sequences(_on_gpu(table, torch.int32, shape, gpu, "table"),
+                     _on_gpu(lengths, torch.int32, (n,), gpu, "lengths"),
+                     _on_gpu(token_offsets, torch.int32, (n + 1,), gpu, "token_offsets"),
                      n, pages, n_tokens, max_tokens)
 
 
@@ -508,7 +519,7 @@ def rm_w4_linear(x, codes, scales, group, zeros=None, bias=None, act="none", out
     be strided), even elements in the low half; scales [n, ceil(k / group)] of
     x's type; zeros uint8 like scales (None: 8); bias [n].  act "swiglu" takes
     the first half of the outputs as gates of the second."""
-    kind, dtype = _type_of(x, "x"), x.dtype
+    (kind, gpu), dtype = _type_of(x, "x"), x.dtype
     if x.dim() != 2 or codes.dim() != 2:
         raise ValueError("rm_w4_linear: expected x [rows, k] and codes [n, ceil(k / 2)]")
     rows, k = shape = x.shape
@@ -523,22 +534,22 @@ def rm_w4_linear(x, codes, scales, group, zeros=None, bias=None, act="none", out
         out = x.new_empty((rows, width))
         out_pitch = width
     else:
-        out_pitch = _pitch(_rows(out, dtype, (rows, width), "out")[0], rows, width, "out")
-    x_pitch = _pitch(_rows(x, dtype, shape, "x")[0], rows, k, "x")
-    code_pitch = _pitch(_rows(codes, torch.uint8, (n, row_bytes), "codes")[0], n, row_bytes,
+        out_pitch = _pitch(_rows(out, dtype, (rows, width), gpu, "out")[0], rows, width, "out")
+    x_pitch = _pitch(_rows(x, dtype, shape, gpu, "x")[0], rows, k, "x")
+    code_pitch = _pitch(_rows(codes, torch.uint8, (n, row_bytes), gpu, "codes")[0], n, row_bytes,
                         "codes")
     args = (kind, rows, n, k, x.data_ptr(), x_pitch, codes.data_ptr(), code_pitch, group,
-            _on_gpu(scales, dtype, groups, "scales"),
-            _on_gpu(zeros, torch.uint8, groups, "zeros"),
-            _on_gpu(bias, dtype, (n,), "bias"), act, out.data_ptr(), out_pitch)
-    lib, stream = _lib or library(), _raw_stream(x.get_device())
+            _on_gpu(scales, dtype, groups, gpu, "scales"),
+            _on_gpu(zeros, torch.uint8, groups, gpu, "zeros"),
+            _on_gpu(bias, dtype, (n,), gpu, "bias"), act, out.data_ptr(), out_pitch)
+    lib = _lib or library()
     if workspace is None:
-        code = lib.rm_w4_linear(*args, None, 0, stream)
+        code = _call(lib.rm_w4_linear, gpu, *args, None, 0)
         if code == RM_EWORKSPACE:     # most sizes need none, so it is asked for only then
             workspace = torch.empty(lib.rm_w4_linear_workspace_bytes(rows, n, k, act),
                                     dtype=torch.uint8, device=x.device)
     if workspace is not None:
-        code = lib.rm_w4_linear(*args, workspace.data_ptr(), workspace.numel(), stream)
+        code = _call(lib.rm_w4_linear, gpu, *args, workspace.data_ptr(), workspace.numel())
     if code:
         _check(code, "rm_w4_linear")
     return out
@@ -551,33 +562,34 @@ def rm_rotary_append(q, k, v, inv_freq, cache, table, lengths, token_offsets=Non
     appends k and v to the cache, whose `lengths` count the call's tokens
     already.  q, k and v may be views of one projection.  Returns the turned
     q (None for q None)."""
-    kind, dtype = _type_of(k, "k"), k.dtype
-    c = _cache_of(cache)
+    (kind, gpu), dtype = _type_of(k, "k"), k.dtype
+    c = _cache_of(cache, gpu)
     if k.dim() != 3:
         raise ValueError("k: expected [tokens, kv_heads, head_dim]")
     tokens, dim = k.shape[0], c.head_dim
     shape = (tokens, c.kv_heads, dim)
-    s = _sequences_of(table, lengths, token_offsets, tokens, max_tokens)
-    ks, vs = _rows(k, dtype, shape, "k"), _rows(v, dtype, shape, "v")
+    s = _sequences_of(table, lengths, token_offsets, tokens, max_tokens, gpu)
+    ks, vs = _rows(k, dtype, shape, gpu, "k"), _rows(v, dtype, shape, gpu, "v")
     heads, qp, qs, op = 0, None, (0, 0), None
     if q is not None:
         if q.dim() != 3:
             raise ValueError("q: expected [tokens, heads, head_dim]")
         heads = q.shape[1]
         shape = (tokens, heads, dim)
-        qs, qp = _rows(q, dtype, shape, "q"), q.data_ptr()
+        qs, qp = _rows(q, dtype, shape, gpu, "q"), q.data_ptr()
         if q_out is None:
             q_out = k.new_empty(shape)
             op = q_out.data_ptr()
         else:
-            op = _on_gpu(q_out, dtype, shape, "q_out")
+            op = _on_gpu(q_out, dtype, shape, gpu, "q_out")
     half = inv_freq.numel()
-    code = (_lib or library()).rm_rotary_append(
+    code = _call(
+        (_lib or library()).rm_rotary_append, gpu,
         kind, c, s, heads, qp, qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0],
-        vs[1], _on_gpu(positions, torch.int32, (tokens,), "positions"),
-        _on_gpu(inv_freq, torch.float32, (half,), "inv_freq"), 2 * half,
+        vs[1], _on_gpu(positions, torch.int32, (tokens,), gpu, "positions"),
+        _on_gpu(inv_freq, torch.float32, (half,), gpu, "inv_freq"), 2 * half,
         _named(ROTARY_NAMES, layout, "layout"), rot_scale, op,
-        _on_gpu(status, torch.int32, (1,), "status"), _raw_stream(k.get_device()))
+        _on_gpu(status, torch.int32, (1,), gpu, "status"))
     if code:
         _check(code, "rm_rotary_append")
     return q_out
@@ -586,7 +598,10 @@ def rm_rotary_append(q, k, v, inv_freq, cache, table, lengths, token_offsets=Non
 def rm_cache_read(cache, pages, dtype=torch.bfloat16, status=None):
     """Keys and values that `pages` (int32) hold: two tensors [pages,
     page_tokens, kv_heads, head_dim]."""
-    c = _cache_of(cache)
+    gpu = pages.get_device()
+    if gpu < 0:
+        raise ValueError(f"pages: expected a GPU tensor, got one on {pages.device}")
+    c = _cache_of(cache, gpu)
     n = pages.numel()
     kind = TYPES.get(dtype)
     if kind is None:
@@ -594,9 +609,10 @@ def rm_cache_read(cache, pages, dtype=torch.bfloat16, status=None):
     both = torch.empty((2, n, c.page_tokens, c.kv_heads, c.head_dim), dtype=dtype,
                        device=pages.device)
     k, v = both.unbind()
-    code = (_lib or library()).rm_cache_read(
-        kind, c, n, _on_gpu(pages, torch.int32, (n,), "pages"), k.data_ptr(), v.data_ptr(),
-        _on_gpu(status, torch.int32, (1,), "status"), _raw_stream(pages.get_device()))
+    code = _call(
+        (_lib or library()).rm_cache_read, gpu,
+        kind, c, n, _on_gpu(pages, torch.int32, (n,), gpu, "pages"), k.data_ptr(), v.data_ptr(),
+        _on_gpu(status, torch.int32, (1,), gpu, "status"))
     if code:
         _check(code, "rm_cache_read")
     return k, v
@@ -606,13 +622,13 @@ def rm_cache_attention(q, cache, table, lengths, token_offsets=None, max_tokens=
                        window=0, workspace=None, out=None, status=None):
     """Attention of q [tokens, heads, dim] over the cache (causal; `window` > 0
     keeps each token's last `window`).  scale None: 1 / sqrt(dim)."""
-    kind, dtype = _type_of(q, "q"), q.dtype
-    c = _cache_of(cache)
+    (kind, gpu), dtype = _type_of(q, "q"), q.dtype
+    c = _cache_of(cache, gpu)
     if q.dim() != 3:
         raise ValueError("q: expected [tokens, heads, head_dim]")
     tokens, heads, dim = shape = q.shape
-    qs = _rows(q, dtype, (tokens, heads, c.head_dim), "q")
-    s = _sequences_of(table, lengths, token_offsets, tokens, max_tokens)
+    qs = _rows(q, dtype, (tokens, heads, c.head_dim), gpu, "q")
+    s = _sequences_of(table, lengths, token_offsets, tokens, max_tokens, gpu)
     lib = _lib or library()
     if workspace is None:
         need = lib.rm_cache_attention_workspace_bytes(c, s, heads)
@@ -623,11 +639,12 @@ def rm_cache_attention(q, cache, table, lengths, token_offsets=None, max_tokens=
         out = q.new_empty(shape)
         op = out.data_ptr()
     else:
-        op = _on_gpu(out, dtype, shape, "out")
-    code = lib.rm_cache_attention(
+        op = _on_gpu(out, dtype, shape, gpu, "out")
+    code = _call(
+        lib.rm_cache_attention, gpu,
         kind, c, s, heads, q.data_ptr(), qs[0], qs[1], dim ** -0.5 if scale is None else scale,
         window, op, workspace.data_ptr(), workspace.numel(),
-        _on_gpu(status, torch.int32, (1,), "status"), _raw_stream(q.get_device()))
+        _on_gpu(status, torch.int32, (1,), gpu, "status"))
     if code:
         _check(code, "rm_cache_attention")
     return out
@@ -639,23 +656,23 @@ def rm_norm_residual(x, y=None, gate=None, post_weight=None, pre_weight=None, pr
     where that is given; n = x' normalised times pre_weight plus pre_bias.
     x, y [rows, width]; gate [width], [rows, 1] or [rows, width].  Without y
     x' is x itself."""
-    code_type, dtype = _type_of(x, "x"), x.dtype
+    (code_type, gpu), dtype = _type_of(x, "x"), x.dtype
     if x.dim() != 2:
         raise ValueError("x: expected [rows, width]")
     rows, width = shape = x.shape
-    x_pitch = _pitch(_rows(x, dtype, shape, "x")[0], rows, width, "x")
+    x_pitch = _pitch(_rows(x, dtype, shape, gpu, "x")[0], rows, width, "x")
     yp, y_pitch = None, 0
     if y is not None:
-        y_pitch = _pitch(_rows(y, dtype, shape, "y")[0], rows, width, "y")
+        y_pitch = _pitch(_rows(y, dtype, shape, gpu, "y")[0], rows, width, "y")
         yp = y.data_ptr()
     gp, gs, gw = None, 0, 0
     if gate is not None:
         if gate.dim() == 1:
-            gp, gw = _on_gpu(gate, dtype, (width,), "gate"), width
+            gp, gw = _on_gpu(gate, dtype, (width,), gpu, "gate"), width
         else:
             gw = gate.shape[1]
-            gs = _rows(gate, dtype, (rows, gw), "gate")[0] if rows > 1 else 0
-            gp = gate.data_ptr() if rows > 1 else _on_gpu(gate, dtype, (rows, gw), "gate")
+            gs = _rows(gate, dtype, (rows, gw), gpu, "gate")[0] if rows > 1 else 0
+            gp = gate.data_ptr() if rows > 1 else _on_gpu(gate, dtype, (rows, gw), gpu, "gate")
     whole = x.is_contiguous()        # empty_like takes two thirds of new_empty's time
     if x_out is None:
         if y is None:
@@ -664,18 +681,19 @@ def rm_norm_residual(x, y=None, gate=None, post_weight=None, pre_weight=None, pr
             x_out = torch.empty_like(x) if whole else x.new_empty(shape)
             xo = x_out.data_ptr()
     else:
-        xo = _on_gpu(x_out, dtype, shape, "x_out")
+        xo = _on_gpu(x_out, dtype, shape, gpu, "x_out")
     if n_out is None:
         n_out = torch.empty_like(x) if whole else x.new_empty(shape)
         no = n_out.data_ptr()
     else:
-        no = _on_gpu(n_out, dtype, shape, "n_out")
+        no = _on_gpu(n_out, dtype, shape, gpu, "n_out")
     wide = (width,)
-    code = (_lib or library()).rm_norm_residual(
+    code = _call(
+        (_lib or library()).rm_norm_residual, gpu,
         code_type, _named(NORM_NAMES, kind, "kind"), rows, width, x.data_ptr(), x_pitch, yp,
-        y_pitch, gp, gs, gw, _on_gpu(post_weight, dtype, wide, "post_weight"),
-        _on_gpu(pre_weight, dtype, wide, "pre_weight"), _on_gpu(pre_bias, dtype, wide, "pre_bias"),
-        alpha, eps, xo, no, _raw_stream(x.get_device()))
+        y_pitch, gp, gs, gw, _on_gpu(post_weight, dtype, wide, gpu, "post_weight"),
+        _on_gpu(pre_weight, dtype, wide, gpu, "pre_weight"),
+        _on_gpu(pre_bias, dtype, wide, gpu, "pre_bias"), alpha, eps, xo, no)
     if code:
         _check(code, "rm_norm_residual")
     return x_out, n_out

@@ -1,0 +1,150 @@
+"""What the binding of the decode-layer operators hands to the library, seen with
+stand-ins for tensors on two GPUs and for the library: which GPU a call goes to,
+and what it refuses.  These need no GPU."""
+import contextlib
+
+import pytest
+import torch
+
+from paper_2607_16784_amd import api
+
+BF16, F32, I32, U8, I8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8, torch.int8
+
+
+class Tensor:
+    def __init__(self, shape, dtype, gpu=1, strides=None):
+        self.shape, self.dtype, self.gpu = torch.Size(shape), dtype, gpu
+        dense = [1] * len(shape)
+        for i in range(len(shape) - 2, -1, -1):
+            dense[i] = dense[i + 1] * shape[i + 1]
+        self.strides, self.dense = tuple(strides or dense), tuple(dense)
+
+    is_cuda = property(lambda t: t.gpu >= 0)
+    device = property(lambda t: f"cuda:{t.gpu}" if t.gpu >= 0 else "cpu")
+    get_device = lambda t: t.gpu                                     # noqa: E731
+    dim = lambda t: len(t.shape)                                     # noqa: E731
+    stride = lambda t: t.strides                                     # noqa: E731
+    is_contiguous = lambda t: t.strides == t.dense                   # noqa: E731
+    data_ptr = lambda t: 4096                                        # noqa: E731
+    numel = lambda t: t.shape.numel()                                # noqa: E731
+    element_size = lambda t: torch.empty(0, dtype=t.dtype).element_size()   # noqa: E731
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """(entry point, current GPU, its arguments) of every call."""
+    made, current = [], [0]
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*args):
+                if name.endswith("_bytes"):
+                    return 256
+                made.append((name, current[0], args))
+                return 0
+            return call
+
+    @contextlib.contextmanager
+    def device(gpu):
+        before, current[0] = current[0], gpu
+        yield
+        current[0] = before
+
+    monkeypatch.setattr(api, "_lib", Library())
+    monkeypatch.setattr(api, "_raw_stream", lambda gpu: 1000 + gpu)
+    monkeypatch.setattr(api, "_current_gpu", lambda: current[0], raising=False)
+    monkeypatch.setattr(torch.cuda, "device", device)
+    return made
+
+
+def cache():
+    return {"k": Tensor((4, 2, 16, 64), I8), "v": Tensor((4, 2, 64, 16), I8),
+            "k_scale": Tensor((4, 2), F32), "v_scale": Tensor((4, 2), F32)}
+
+
+def linear():
+    return api.rm_w4_linear, dict(
+        x=Tensor((3, 64), BF16), codes=Tensor((8, 32), U8), scales=Tensor((8, 2), BF16), group=32,
+        zeros=Tensor((8, 2), U8), bias=Tensor((8,), BF16), out=Tensor((3, 8), BF16),
+        workspace=Tensor((512,), U8))
+
+
+def append():
+    return api.rm_rotary_append, dict(
+        q=Tensor((3, 4, 64), BF16), k=Tensor((3, 2, 64), BF16), v=Tensor((3, 2, 64), BF16),
+        inv_freq=Tensor((32,), F32), cache=cache(), table=Tensor((2, 2), I32),
+        lengths=Tensor((2,), I32), token_offsets=Tensor((3,), I32), max_tokens=2,
+        positions=Tensor((3,), I32), q_out=Tensor((3, 4, 64), BF16), status=Tensor((1,), I32))
+
+
+def attention():
+    return api.rm_cache_attention, dict(
+        q=Tensor((3, 4, 64), BF16), cache=cache(), table=Tensor((2, 2), I32),
+        lengths=Tensor((2,), I32), token_offsets=Tensor((3,), I32), max_tokens=2,
+        workspace=Tensor((512,), U8), out=Tensor((3, 4, 64), BF16), status=Tensor((1,), I32))
+
+
+def norm():
+    return api.rm_norm_residual, dict(
+        x=Tensor((3, 64), BF16), y=Tensor((3, 64), BF16), gate=Tensor((3, 1), BF16),
+        post_weight=Tensor((64,), BF16), pre_weight=Tensor((64,), BF16),
+        pre_bias=Tensor((64,), BF16), x_out=Tensor((3, 64), BF16), n_out=Tensor((3, 64), BF16))
+
+
+CALLS = [linear, append, attention, norm]
+
+
+@pytest.mark.parametrize("make", CALLS)
+def test_a_call_goes_to_the_gpu_of_its_tensors(calls, make):
+    f, kw = make()
+    f(**kw)
+    (name, gpu, args), = calls
+    assert name == f.__name__ and gpu == 1 and args[-1] == 1001
+    with torch.cuda.device(1):
+        f(**kw)
+    assert calls[1][1] == 1 and calls[1][2][-1] == 1001
+
+
+@pytest.mark.parametrize("make", CALLS)
+@pytest.mark.parametrize("gpu", [0, -1])
+def test_all_tensors_of_a_call_are_on_one_gpu(calls, make, gpu):
+    f, kw = make()
+    names = [n for n, t in kw.items() if isinstance(t, Tensor) and n != "workspace"]
+    names += [("cache", n) for n in kw.get("cache", {})]
+    assert len(names) > 5
+    for n in names:
+        _, bad = make()
+        if isinstance(n, tuple):
+            bad["cache"][n[1]].gpu = gpu
+        else:
+            bad[n].gpu = gpu
+        with pytest.raises(ValueError):
+            f(**bad)
+    assert calls == []
+    _, bad = make()
+    if "gate" in bad:
+        bad["gate"] = Tensor((64,), BF16, gpu)
+        with pytest.raises(ValueError):
+            f(**bad)
+
+
+def test_cache_read_goes_to_the_gpu_of_its_tensors(calls, monkeypatch):
+    pages = Tensor((2,), I32)
+    both = type("Both", (), {"unbind": lambda t: (Tensor((2, 16, 2, 64), BF16),) * 2})()
+    monkeypatch.setattr(api.torch, "empty", lambda *a, **kw: both)
+    api.rm_cache_read(cache(), pages)
+    assert calls[0][1] == 1 and calls[0][2][-1] == 1001
+    for n in cache():
+        bad = cache()
+        bad[n].gpu = 0
+        with pytest.raises(ValueError):
+            api.rm_cache_read(bad, pages)
+    for gpu in (0, -1):
+        with pytest.raises(ValueError):
+            api.rm_cache_read(cache(), Tensor((2,), I32, gpu))
+    every = cache()
+    for t in every.values():
+        t.gpu = -1
+    with pytest.raises(ValueError):
+        api.rm_cache_read(every, Tensor((2,), I32, -1))
+    assert len(calls) == 1
