@@ -437,6 +437,14 @@ def _rows(t, dtype, shape, gpu, name):
                      f"cuda:{gpu}, got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
+def _scratch(t, gpu):
+    """Address and bytes of a caller's workspace."""
+    if t.get_device() == gpu and t.is_contiguous():
+        return t.data_ptr(), t.numel() * t.element_size()
+    raise ValueError(f"workspace: expected a contiguous tensor on cuda:{gpu}, got strides "
+                     f"{t.stride()} on {t.device}")
+
+
 def _pitch(stride, rows, width, name):
     """Elements between rows; rows may not overlap."""
     if rows <= 1:
@@ -549,7 +557,7 @@ def rm_w4_linear(x, codes, scales, group, zeros=None, bias=None, act="none", out
             workspace = torch.empty(lib.rm_w4_linear_workspace_bytes(rows, n, k, act),
                                     dtype=torch.uint8, device=x.device)
     if workspace is not None:
-        code = _call(lib.rm_w4_linear, gpu, *args, workspace.data_ptr(), workspace.numel())
+        code = _call(lib.rm_w4_linear, gpu, *args, *_scratch(workspace, gpu))
     if code:
         _check(code, "rm_w4_linear")
     return out
@@ -643,7 +651,7 @@ def rm_cache_attention(q, cache, table, lengths, token_offsets=None, max_tokens=
     code = _call(
         lib.rm_cache_attention, gpu,
         kind, c, s, heads, q.data_ptr(), qs[0], qs[1], dim ** -0.5 if scale is None else scale,
-        window, op, workspace.data_ptr(), workspace.numel(),
+        window, op, *_scratch(workspace, gpu),
         _on_gpu(status, torch.int32, (1,), gpu, "status"))
     if code:
         _check(code, "rm_cache_attention")

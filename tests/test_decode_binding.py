@@ -148,3 +148,24 @@ def test_cache_read_goes_to_the_gpu_of_its_tensors(calls, monkeypatch):
     with pytest.raises(ValueError):
         api.rm_cache_read(every, Tensor((2,), I32, -1))
     assert len(calls) == 1
+
+
+@pytest.mark.parametrize("make", [linear, attention])
+@pytest.mark.parametrize("workspace", [Tensor((512,), U8, gpu=-1), Tensor((512,), U8, gpu=0),
+                                       Tensor((512,), U8, strides=(2,)),
+                                       Tensor((8, 64), U8, strides=(128, 1))])
+def test_a_workspace_that_no_kernel_may_write(calls, make, workspace):
+    f, kw = make()
+    with pytest.raises(ValueError, match="workspace"):
+        f(**dict(kw, workspace=workspace))
+    assert calls == []
+
+
+@pytest.mark.parametrize("make", [linear, attention])
+def test_a_workspace_counts_in_bytes(calls, make):
+    f, kw = make()
+    f(**dict(kw, workspace=Tensor((256,), F32)))
+    f(**dict(kw, workspace=Tensor((8, 128), torch.float64)))
+    # the size stands behind the workspace's address
+    sizes = [args[-2] if f.__name__ == "rm_w4_linear" else args[-3] for _, _, args in calls]
+    assert sizes == [1024, 8192]
