@@ -470,6 +470,19 @@ def _named(names, value, what):
     return code
 
 
+# ctypes takes the low 32 bits of a larger number without a word.
+
+def _int32(value, name):
+    if -1 << 31 <= value < 1 << 31:
+        return value
+    raise ValueError(f"{name}: {value} does not fit 32 bits")
+
+
+def _sizes_fit(*sizes):
+    if max(sizes) >> 31:
+        raise ValueError(f"sizes beyond 31 bits: {sizes}")
+
+
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _current_gpu = getattr(torch._C, "_cuda_getDevice", None)
 
@@ -515,10 +528,12 @@ def _sequences_of(table, lengths, token_offsets, n_tokens, max_tokens, gpu):
     if table.dim() != 2:
         raise ValueError("table: expected [sequences, pages]")
     n, pages = shape = table.shape
+    if (n | pages | n_tokens) >> 31:
+        _sizes_fit(n, pages, n_tokens)
     return Sequences(_on_gpu(table, torch.int32, shape, gpu, "table"),
                      _on_gpu(lengths, torch.int32, (n,), gpu, "lengths"),
                      _on_gpu(token_offsets, torch.int32, (n + 1,), gpu, "token_offsets"),
-                     n, pages, n_tokens, max_tokens)
+                     n, pages, n_tokens, _int32(max_tokens, "max_tokens"))
 
 
 def rm_w4_linear(x, codes, scales, group, zeros=None, bias=None, act="none", out=None,
@@ -534,6 +549,8 @@ def rm_w4_linear(x, codes, scales, group, zeros=None, bias=None, act="none", out
     n = codes.shape[0]
     if group < 1 or group % 32:
         raise ValueError(f"group: expected a multiple of 32, got {group}")
+    if (rows | n | k | group) >> 31:
+        _sizes_fit(rows, n, k, group)
     row_bytes = (k + 1) // 2
     groups = (n, -(-k // group))
     act = _named(ACT_NAMES, act, "act")
@@ -611,6 +628,8 @@ def rm_cache_read(cache, pages, dtype=torch.bfloat16, status=None):
         raise ValueError(f"pages: expected a GPU tensor, got one on {pages.device}")
     c = _cache_of(cache, gpu)
     n = pages.numel()
+    if n >> 31:
+        _sizes_fit(n)
     kind = TYPES.get(dtype)
     if kind is None:
         raise ValueError(f"dtype: expected bfloat16 or float16, got {dtype}")
@@ -651,7 +670,7 @@ def rm_cache_attention(q, cache, table, lengths, token_offsets=None, max_tokens=
     code = _call(
         lib.rm_cache_attention, gpu,
         kind, c, s, heads, q.data_ptr(), qs[0], qs[1], dim ** -0.5 if scale is None else scale,
-        window, op, *_scratch(workspace, gpu),
+        _int32(window, "window"), op, *_scratch(workspace, gpu),
         _on_gpu(status, torch.int32, (1,), gpu, "status"))
     if code:
         _check(code, "rm_cache_attention")
@@ -668,6 +687,8 @@ def rm_norm_residual(x, y=None, gate=None, post_weight=None, pre_weight=None, pr
     if x.dim() != 2:
         raise ValueError("x: expected [rows, width]")
     rows, width = shape = x.shape
+    if (rows | width) >> 31:
+        _sizes_fit(rows, width)
     x_pitch = _pitch(_rows(x, dtype, shape, gpu, "x")[0], rows, width, "x")
     yp, y_pitch = None, 0
     if y is not None:

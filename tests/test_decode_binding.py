@@ -169,3 +169,55 @@ def test_a_workspace_counts_in_bytes(calls, make):
     # the size stands behind the workspace's address
     sizes = [args[-2] if f.__name__ == "rm_w4_linear" else args[-3] for _, _, args in calls]
     assert sizes == [1024, 8192]
+
+
+BEYOND = [1 << 31, (1 << 32) + 32, -(1 << 32) + 32, -(1 << 31) - 1]
+
+
+@pytest.mark.parametrize("value", BEYOND)
+def test_numbers_beyond_32_bits_are_refused(calls, value):
+    # the C entry points take int32: 2^32 + 32 would arrive as 32
+    f, kw = linear()
+    with pytest.raises(ValueError):
+        f(**dict(kw, group=value, scales=Tensor((8, 1), BF16), zeros=Tensor((8, 1), U8)))
+    f, kw = attention()
+    for name in ("window", "max_tokens"):
+        with pytest.raises(ValueError, match=name):
+            f(**dict(kw, **{name: value}))
+    f, kw = append()
+    with pytest.raises(ValueError, match="max_tokens"):
+        f(**dict(kw, max_tokens=value))
+    assert calls == []
+
+
+def test_sizes_beyond_32_bits_are_refused(calls):
+    many = (1 << 32) + 3
+    f, kw = linear()
+    with pytest.raises(ValueError, match="sizes"):
+        f(**dict(kw, x=Tensor((many, 64), BF16), out=Tensor((many, 8), BF16)))
+    f, kw = norm()
+    wide = {n: Tensor((many, 64), BF16) for n in ("x", "y", "x_out", "n_out")}
+    with pytest.raises(ValueError, match="sizes"):
+        f(**dict(kw, gate=None, **wide))
+    f, kw = attention()
+    with pytest.raises(ValueError, match="sizes"):
+        f(**dict(kw, table=Tensor((2, many), I32)))
+    with pytest.raises(ValueError, match="sizes"):
+        f(**dict(kw, q=Tensor((many, 4, 64), BF16), out=Tensor((many, 4, 64), BF16)))
+    f, kw = append()
+    tall = {n: Tensor((many, 4, 64), BF16) for n in ("q", "q_out")}
+    tall |= {n: Tensor((many, 2, 64), BF16) for n in ("k", "v")}
+    with pytest.raises(ValueError, match="sizes"):
+        f(**dict(kw, positions=None, **tall))
+    with pytest.raises(ValueError, match="sizes"):
+        api.rm_cache_read(cache(), Tensor((many,), I32))
+    assert calls == []
+
+
+def test_the_largest_numbers_pass(calls):
+    f, kw = attention()
+    f(**dict(kw, window=(1 << 31) - 1, max_tokens=(1 << 31) - 1))
+    f(**dict(kw, window=-1))            # the library's to refuse
+    f, kw = linear()
+    f(**dict(kw, group=(1 << 31) - 32, scales=Tensor((8, 1), BF16), zeros=Tensor((8, 1), U8)))
+    assert len(calls) == 3
