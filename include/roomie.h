@@ -122,7 +122,7 @@ extern "C" {
 
 #define RM_MAX_NORM_WIDTH    32768  /* width of rm_norm_residual               */
 #define RM_MAX_W4_COLUMNS  2097152  /* k of rm_w4_linear                       */
-#define RM_MAX_W4_OUTPUTS 1073741824 /* n of rm_w4_linear                      */
+#define RM_MAX_W4_OUTPUTS 536870848 /* n of rm_w4_linear                       */
 #define RM_MAX_W4_ROWS     4194240  /* rows of rm_w4_linear                    */
 #define RM_MAX_SEQUENCES     65535  /* n_seqs of the cache calls               */
 
@@ -560,7 +560,8 @@ int rm_w4_linear(int32_t type, int32_t rows, int32_t n, int32_t k, const void* x
  * heads may be 0 (q and q_out are then not read).
  * Errors: RM_EINVAL (NULL pointer, negative size, rot odd or > head_dim, bad
  *   type, layout or codes), RM_EUNSUPPORTED (page_tokens or head_dim not
- *   listed, n_seqs over RM_MAX_SEQUENCES, heads or kv_heads over 65535),
+ *   listed, n_seqs over RM_MAX_SEQUENCES, heads or kv_heads over 65535, pages
+ *   of max_tokens over all sequences and heads beyond 2^31 workgroups),
  *   RM_ELAUNCH.
  */
 int rm_rotary_append(int32_t type, const rm_cache* cache, const rm_sequences* seqs,
@@ -596,8 +597,9 @@ int rm_cache_read(int32_t type, const rm_cache* cache, int32_t n, const int32_t*
  * A page id out of range is reported where some token sees the page.
  * workspace: rm_cache_attention_workspace_bytes bytes, 256-byte aligned.
  * Errors: RM_EINVAL (also heads not a multiple of kv_heads, scale not finite,
- *   window < 0), RM_EUNSUPPORTED (also max_tokens * heads / kv_heads beyond 31
- *   bits), RM_EWORKSPACE, RM_ELAUNCH.
+ *   window < 0), RM_EUNSUPPORTED (also max_tokens * heads / kv_heads, or that
+ *   over 16 for each sequence and kv head, beyond 31 bits), RM_EWORKSPACE,
+ *   RM_ELAUNCH.
  */
 size_t rm_cache_attention_workspace_bytes(const rm_cache* cache, const rm_sequences* seqs,
                                           int32_t heads);

@@ -160,7 +160,7 @@ __device__ inline void clear_rows(const AttendArgs& a, int group)
 template <typename T, int FMT, int D, int C>
 __global__ __launch_bounds__(kWaves * 64)
 __attribute__((amdgpu_waves_per_eu(D <= 128 ? 2 : 1))) void
-attend_kernel(AttendArgs a, Plan plan)
+attend_kernel(AttendArgs a, Plan plan, int64_t first)
 {
     typedef typename Vec<T>::x8 V;
     constexpr int H = 16 * C, W = kWaves;      // rows of a tile
@@ -168,7 +168,7 @@ attend_kernel(AttendArgs a, Plan plan)
     __shared__ float join_m[W][H], join_l[W][H];
 
     const int KV = a.cache.kv_heads, TK = a.cache.page_tokens, G = a.heads / KV;
-    const int64_t part_at = blockIdx.x;
+    const int64_t part_at = first + blockIdx.x;
     if (part_at >= plan.parts) {
         clear_rows<T, D>(a, (int)(part_at - plan.parts));
         return;
@@ -545,8 +545,7 @@ int columns_of(int64_t rows)
 
 Plan plan_of(const rm_cache& c, const rm_sequences& s, int32_t heads)
 {
-    // a tile a sequence at least: it reports one that is out of range
-    const int64_t rows = (int64_t)(s.max_tokens > 1 ? s.max_tokens : 1) * (heads / c.kv_heads);
+    const int64_t rows = most_tokens(s) * (heads / c.kv_heads);
     Plan p;
     p.columns = columns_of(rows);
     const int height = 16 * p.columns;
@@ -574,8 +573,7 @@ template <typename T, int FMT, int D, int C>
 hipError_t launch_columns(const AttendArgs& a, const Plan& p, hipStream_t s)
 {
     const int64_t blocks = p.parts + p.clear, rows = p.parts / p.splits * p.rows;
-    if (blocks == 0) return hipSuccess;
-    if (blocks > 0x7fffffff || rows > 0x7fffffff) return hipErrorInvalidValue;
+    constexpr int64_t most = most_blocks(kWaves * 64);
     const size_t lds = (size_t)(kWaves / 2) * 16 * C * D * sizeof(float);    // 64 KB at most
     const auto kernel = attend_kernel<T, FMT, D, C>;
     if (lds > 60 * 1024) {      // with the static arrays over 64 KB
@@ -584,7 +582,10 @@ hipError_t launch_columns(const AttendArgs& a, const Plan& p, hipStream_t s)
                                                  (int)lds);
         if (e != hipSuccess) return e;
     }
-    hipError_t e = launch(kernel, dim3((unsigned)blocks), kWaves * 64, lds, s, a, p);
+    hipError_t e = hipSuccess;
+    for (int64_t first = 0; first < blocks && e == hipSuccess; first += most)
+        e = launch(kernel, dim3((unsigned)(blocks - first < most ? blocks - first : most)),
+                   kWaves * 64, lds, s, a, p, first);
     if (e != hipSuccess || p.splits == 1 || rows == 0) return e;
     return launch(attend_join_kernel<T, D, C>, dim3((unsigned)rows), 256, 0, s, a, p);
 }
@@ -607,6 +608,12 @@ hipError_t launch_codes(const AttendArgs& a, hipStream_t s)
 }
 
 }  // namespace
+
+bool attend_fits(const rm_cache& c, const rm_sequences& s, int32_t heads)
+{
+    const Plan p = plan_of(c, s, heads);
+    return p.parts + p.clear <= kMostBlocks;
+}
 
 size_t attend_workspace(const rm_cache& c, const rm_sequences& s, int32_t heads)
 {

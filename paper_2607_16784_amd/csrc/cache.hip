@@ -214,13 +214,14 @@ __device__ inline void turn_queries(const AppendArgs& a, int32_t token, int part
 template <typename T, int FMT>
 __global__ __launch_bounds__(1024) void append_kernel(AppendArgs a, int32_t q_blocks,
                                                       int32_t q_parts, int32_t pages_a_seq,
-                                                      int32_t group)
+                                                      int32_t group, int64_t first)
 {
     __shared__ float2 turn[16][kMostPairs];
     __shared__ float part[16];
-    if ((int)blockIdx.x < q_blocks) {
+    const int64_t index = first + blockIdx.x;
+    if (index < q_blocks) {
         const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-        const int64_t at = (int64_t)blockIdx.x * waves + wave, token = at / q_parts;
+        const int64_t at = index * waves + wave, token = at / q_parts;
         if (token < a.seqs.n_tokens)
             turn_queries<T>(a, (int32_t)token, (int)(at % q_parts), q_parts, turn[wave]);
         return;
@@ -230,7 +231,7 @@ __global__ __launch_bounds__(1024) void append_kernel(AppendArgs a, int32_t q_bl
     const int TK = a.cache.page_tokens, D = a.cache.head_dim, KV = a.cache.kv_heads;
     const int groups = blockDim.x / group, sides = 2 * KV;
     const int per_page = (sides + groups - 1) / groups;
-    int64_t at = (int64_t)blockIdx.x - q_blocks;
+    int64_t at = index - q_blocks;
     const int part_of = (int)(at % per_page);
     at /= per_page;
     const int page_no = (int)(at % pages_a_seq), b = (int)(at / pages_a_seq);
@@ -461,39 +462,59 @@ __global__ __launch_bounds__(256) void cache_read_kernel(rm_cache c, int32_t n,
 
 }  // namespace
 
-hipError_t launch_append(int type, const AppendArgs& a, hipStream_t s)
+namespace {
+
+// How an append is laid out.
+struct AppendPlan {
+    int group, threads;       // threads a (page, head, side), and a workgroup
+    int32_t pages, q_parts;   // pages a sequence, waves a token for its queries
+    int64_t q_blocks, blocks;
+};
+
+AppendPlan append_plan(const rm_cache& c, const rm_sequences& s, int32_t heads)
 {
-    const int TK = a.cache.page_tokens;
-    // one a sequence at least: it reports one that is out of range
-    const int64_t most = a.seqs.max_tokens > 1 ? a.seqs.max_tokens : 1;
-    const int32_t pages = (int32_t)((most + 2 * TK - 2) / TK);
-    const int tile = TK * a.cache.head_dim / 32;
-    const int group = tile < 64 ? 64 : tile, threads = group < 256 ? 256 : group;
-    const int groups = threads / group, waves = threads / 64;
+    const int TK = c.page_tokens, tile = TK * c.head_dim / 32;
+    AppendPlan p;
+    p.pages = (int32_t)((most_tokens(s) + 2 * TK - 2) / TK);
+    p.group = tile < 64 ? 64 : tile;
+    p.threads = p.group < 256 ? 256 : p.group;
+    const int groups = p.threads / p.group, waves = p.threads / 64;
     // Waves a token: as many as its queries fill once, while all are 16 a CU at
     // most (17 tokens of 64 heads of 256, with the read back: 10.6 us, a wave a
     // token 31.6; 64 tokens of 32 heads of 128: 10.1 and 12.0).
-    const int64_t fill = ((int64_t)a.heads * (a.cache.head_dim / 8) + kAhead * 64 - 1) /
-                         (kAhead * 64);
-    const int64_t room = 16 * kComputeUnits / a.seqs.n_tokens;
-    const int32_t q_parts = (int32_t)(room < 1 ? 1 : room < fill ? room : fill < 1 ? 1 : fill);
-    const int64_t q_blocks = a.heads > 0 ? ((int64_t)a.seqs.n_tokens * q_parts + waves - 1) / waves
-                                         : 0;
-    const int64_t per_page = (2 * (int64_t)a.cache.kv_heads + groups - 1) / groups;
-    const int64_t blocks = q_blocks + (int64_t)a.seqs.n_seqs * pages * per_page;
-    if (blocks == 0) return hipSuccess;
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks);
-#define RM_APPEND(T, FMT) \
-    return launch(append_kernel<T, FMT>, grid, (unsigned)threads, 0, s, a, (int32_t)q_blocks, \
-                  q_parts, pages, (int32_t)group)
-    if (type == RM_TYPE_BF16) {
-        if (a.cache.codes == RM_CODES_INT8) RM_APPEND(bf16, RM_CODES_INT8);
-        RM_APPEND(bf16, RM_CODES_E4M3);
-    }
-    if (a.cache.codes == RM_CODES_INT8) RM_APPEND(f16, RM_CODES_INT8);
-    RM_APPEND(f16, RM_CODES_E4M3);
-#undef RM_APPEND
+    const int64_t fill = ((int64_t)heads * (c.head_dim / 8) + kAhead * 64 - 1) / (kAhead * 64);
+    const int64_t room = 16 * kComputeUnits / s.n_tokens;
+    p.q_parts = (int32_t)(room < 1 ? 1 : room < fill ? room : fill < 1 ? 1 : fill);
+    p.q_blocks = heads > 0 ? ((int64_t)s.n_tokens * p.q_parts + waves - 1) / waves : 0;
+    const int64_t per_page = (2 * (int64_t)c.kv_heads + groups - 1) / groups;
+    p.blocks = p.q_blocks + (int64_t)s.n_seqs * p.pages * per_page;
+    return p;
+}
+
+}  // namespace
+
+bool append_fits(const rm_cache& c, const rm_sequences& s, int32_t heads)
+{
+    return append_plan(c, s, heads).blocks <= kMostBlocks;
+}
+
+hipError_t launch_append(int type, const AppendArgs& a, hipStream_t s)
+{
+    const AppendPlan p = append_plan(a.cache, a.seqs, a.heads);
+    const int64_t most = most_blocks((unsigned)p.threads);
+    auto run = [&](auto kernel) {
+        hipError_t e = hipSuccess;
+        for (int64_t first = 0; first < p.blocks && e == hipSuccess; first += most)
+            e = launch(kernel, dim3((unsigned)(p.blocks - first < most ? p.blocks - first : most)),
+                       (unsigned)p.threads, 0, s, a, (int32_t)p.q_blocks, p.q_parts, p.pages,
+                       (int32_t)p.group, first);
+        return e;
+    };
+    if (type == RM_TYPE_BF16)
+        return a.cache.codes == RM_CODES_INT8 ? run(append_kernel<bf16, RM_CODES_INT8>)
+                                              : run(append_kernel<bf16, RM_CODES_E4M3>);
+    return a.cache.codes == RM_CODES_INT8 ? run(append_kernel<f16, RM_CODES_INT8>)
+                                          : run(append_kernel<f16, RM_CODES_E4M3>);
 }
 
 hipError_t launch_cache_read(int type, const rm_cache& c, int32_t n, const int32_t* pages,

@@ -54,10 +54,12 @@ int check_seqs(const rm_sequences* s, const rm_cache* c)
     return RM_OK;
 }
 
-// (token, head) pairs of a sequence and kv head are counted in 32 bits.
+// (token, head) pairs of a sequence and kv head are counted in 32 bits, and so
+// are the workgroups.
 bool rows_fit(const rm_sequences* s, const rm_cache* c, int32_t heads)
 {
-    return (int64_t)s->max_tokens * (heads / c->kv_heads) <= 0x7fffff00;
+    return (int64_t)s->max_tokens * (heads / c->kv_heads) <= 0x7fffff00 &&
+           attend_fits(*c, *s, heads);
 }
 
 // floor(k / group) = umulhi(k / 32, inverse) for every column below k: the
@@ -140,6 +142,7 @@ int rm_rotary_append(int32_t type, const rm_cache* cache, const rm_sequences* se
     if (seqs->n_tokens == 0) return RM_OK;
     if (cache->n_pages < 1) return RM_EINVAL;
     if (!k || !v || (heads > 0 && (!q || !q_out)) || (rot > 0 && !inv_freq)) return RM_EINVAL;
+    if (!rm::append_fits(*cache, *seqs, heads)) return RM_EUNSUPPORTED;
     rm::AppendArgs a = {*cache, *seqs, heads, rot, layout, q, k, v, q_stride, q_head_stride,
                         k_stride, k_head_stride, v_stride, v_head_stride, positions, inv_freq,
                         rot_scale, q_out, status};

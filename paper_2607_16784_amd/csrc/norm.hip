@@ -190,7 +190,7 @@ hipError_t launch_form(const NormArgs& a, hipStream_t s)
     // than a stride over the rows, 8190 x 5120 with layer norms 95 us, striding 104,
     // 8000 x 2048 24 and 25.  Workgroups of 1024 threads gain more from their gains
     // in registers: 4000 x 16384 114 us striding, 126 so.
-    const int64_t most = threads == 1024 ? 2 * kComputeUnits : 0x7fffffff;
+    const int64_t most = threads == 1024 ? 2 * kComputeUnits : most_blocks(threads);
     return launch(norm_kernel<T, KIND, C, THREADS, TAIL>,
                   dim3((unsigned)(want < most ? want : most)), threads, 0, s, a);
 }

@@ -115,11 +115,15 @@ constexpr int kComputeUnits = 256;   // of an MI355X
 // outside a recording.
 void note_launch(const void* kernel, int64_t blocks, unsigned threads, size_t dynamic_lds);
 
+// A dispatch holds fewer than 2^32 work-items.
+constexpr int64_t most_blocks(unsigned threads) { return 0xffffffffll / threads; }
+
 // Launches `kernel` and records its shape.
 template <typename... P, typename... A>
 inline hipError_t launch(void (*kernel)(P...), dim3 grid, unsigned threads, size_t lds,
                          hipStream_t s, A... args)
 {
+    if (grid.x > most_blocks(threads)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, s, args...);
     const hipError_t e = hipGetLastError();
     if (e == hipSuccess)
@@ -148,6 +152,18 @@ __device__ inline Sequence sequence_of(const rm_sequences& s, int32_t page_token
     q.n = q.bad ? 0 : (int32_t)(n < q.length ? n : q.length);
     if (q.bad) q.length = 0;
     return q;
+}
+
+// The most workgroups that an attention or an append is laid out in; beyond
+// most_blocks they come in several launches.
+constexpr int64_t kMostBlocks = 0x7fffffff;
+
+// New tokens that a sequence of the call can have; 1 at least, so that every
+// sequence has a workgroup that reports one out of range.
+inline int64_t most_tokens(const rm_sequences& s)
+{
+    const int32_t n = s.max_tokens < s.n_tokens ? s.max_tokens : s.n_tokens;
+    return n > 1 ? n : 1;
 }
 
 struct NormArgs {
@@ -186,6 +202,7 @@ struct AppendArgs {
     void* q_out;
     int32_t* status;
 };
+bool append_fits(const rm_cache& c, const rm_sequences& s, int32_t heads);
 hipError_t launch_append(int type, const AppendArgs& a, hipStream_t s);
 hipError_t launch_cache_read(int type, const rm_cache& c, int32_t n, const int32_t* pages,
                              void* k, void* v, int32_t* status, hipStream_t s);
@@ -200,6 +217,7 @@ struct AttendArgs {
     void *out, *workspace;
     int32_t* status;
 };
+bool attend_fits(const rm_cache& c, const rm_sequences& s, int32_t heads);
 size_t attend_workspace(const rm_cache& c, const rm_sequences& s, int32_t heads);
 hipError_t launch_attend(int type, const AttendArgs& a, hipStream_t s);
 
