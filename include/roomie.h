@@ -20,7 +20,7 @@
  *   rm_cache_attention       attention over the cache
  *   rm_norm_residual         gated, scaled residual between two norms
  *   rm_trace_begin, _end     the launch shapes of these calls, as rm_occupancy
- *                            takes them
+ *                            takes them, and their times
  *
  * Conventions shared by every entry point
  *  - Array arguments are DEVICE pointers (hipMalloc memory or the storage of a
@@ -641,9 +641,16 @@ typedef struct {
  * and rm_norm_residual calls is written to records[0..capacity) (host memory)
  * in order; the launches themselves are as always.  rm_trace_end stores the
  * number of launches, which may exceed the capacity, and ends the recording.
- * Errors: RM_EINVAL (NULL, capacity < 0, begin in a recording, end outside).
+ * rm_trace_begin_timed -- the same with the time that each launch takes on the
+ * device, from its first to its last work-item: rm_trace_end waits for the
+ * recorded launches and stores microseconds[0..capacity) (host memory).  Not for
+ * streams in capture.
+ * Errors: RM_EINVAL (NULL, capacity < 0, begin in a recording, end outside),
+ *   RM_ELAUNCH (events that cannot be made or read; a launch recorded with
+ *   times in a capture).
  */
 int rm_trace_begin(rm_launch* records, int32_t capacity);
+int rm_trace_begin_timed(rm_launch* records, float* microseconds, int32_t capacity);
 int rm_trace_end(int32_t* n_launches);
 
 /* Human-readable text for a return code; for RM_ELAUNCH it names the HIP

@@ -133,10 +133,11 @@ def library():
         lib.rm_norm_residual.argtypes = [i32, i32, i32, i32, P, i64, P, i64, P, i64, i32, P, P, P,
                                          f32, f32, P, P, P]
         lib.rm_trace_begin.argtypes = [ctypes.POINTER(Launch), i32]
+        lib.rm_trace_begin_timed.argtypes = [ctypes.POINTER(Launch), ctypes.POINTER(f32), i32]
         lib.rm_trace_end.argtypes = [ctypes.POINTER(i32)]
         for f in (lib.rm_w4_linear, lib.rm_rotary_append, lib.rm_cache_read,
                   lib.rm_cache_attention, lib.rm_norm_residual, lib.rm_trace_begin,
-                  lib.rm_trace_end):
+                  lib.rm_trace_begin_timed, lib.rm_trace_end):
             f.restype = ctypes.c_int
         lib.rm_status_string.argtypes = [ctypes.c_int]
         lib.rm_status_string.restype = ctypes.c_char_p
@@ -730,14 +731,22 @@ def rm_norm_residual(x, y=None, gate=None, post_weight=None, pre_weight=None, pr
 
 class rm_trace:
     """Context manager: the launch shapes of the decode-layer calls inside it,
-    as a list of dicts `launches` (grid, threads, regs, smem) after it."""
+    as a list of dicts `launches` (grid, threads, regs, smem) after it; `timed`
+    adds `duration`, the microseconds that each launch took on the GPU (the end
+    of the block then waits for them; not for graphs in capture)."""
 
-    def __init__(self, capacity=4096):
+    def __init__(self, capacity=4096, timed=False):
         self._records = (Launch * capacity)()
+        self._times = (ctypes.c_float * capacity)() if timed else None
         self.launches = []
 
     def __enter__(self):
-        _check(library().rm_trace_begin(self._records, len(self._records)), "rm_trace_begin")
+        n = len(self._records)
+        if self._times is None:
+            _check(library().rm_trace_begin(self._records, n), "rm_trace_begin")
+        else:
+            _check(library().rm_trace_begin_timed(self._records, self._times, n),
+                   "rm_trace_begin_timed")
         return self
 
     def __exit__(self, *exc):
@@ -747,4 +756,6 @@ class rm_trace:
             raise RuntimeError(f"rm_trace: {n.value} launches, room for {len(self._records)}")
         self.launches = [{f: getattr(r, f) for f, _ in Launch._fields_}
                          for r in self._records[:min(n.value, len(self._records))]]
+        for i, launch in enumerate(self.launches if self._times is not None else ()):
+            launch["duration"] = self._times[i]
         return False

@@ -1,6 +1,7 @@
 // decode_api.hip -- the extern "C" entry points of the decode-layer kernels:
 // host-side argument checks, launches and the record of launch shapes.
 #include <cmath>
+#include <new>
 
 #include "rm_common.h"
 #include "rm_decode.h"
@@ -11,10 +12,24 @@ namespace {
 
 struct Recording {
     rm_launch* records = nullptr;
+    float* microseconds = nullptr;       // nullptr: without times
+    hipEvent_t* events = nullptr;        // start and end of each launch
     int32_t capacity = 0, count = 0;
     bool on = false;
 };
 thread_local Recording g_recording;
+
+int begin(rm_launch* records, float* microseconds, hipEvent_t* events, int32_t capacity)
+{
+    Recording& r = g_recording;
+    r.records = records;
+    r.microseconds = microseconds;
+    r.events = events;
+    r.capacity = capacity;
+    r.count = 0;
+    r.on = true;
+    return RM_OK;
+}
 
 int done(hipError_t e)
 {
@@ -86,6 +101,23 @@ void note_launch(const void* kernel, int64_t blocks, unsigned threads, size_t dy
         l.smem = (int32_t)(dynamic_lds + (known ? f.sharedSizeBytes : 0));
     }
     if (r.count < 0x7fffffff) ++r.count;
+}
+
+hipError_t launch_events(hipStream_t s, hipEvent_t& begin, hipEvent_t& end)
+{
+    begin = end = nullptr;
+    const Recording& r = g_recording;
+    if (!r.events || r.count >= r.capacity) return hipSuccess;
+    hipStreamCaptureStatus capture;
+    hipError_t e = hipStreamIsCapturing(s, &capture);
+    if (e != hipSuccess) return e;
+    if (capture != hipStreamCaptureStatusNone) return hipErrorStreamCaptureUnsupported;
+    hipEvent_t* at = r.events + 2 * (int64_t)r.count;
+    for (int i = 0; i < 2; ++i)
+        if (!at[i] && (e = hipEventCreate(&at[i])) != hipSuccess) return e;
+    begin = at[0];
+    end = at[1];
+    return hipSuccess;
 }
 
 }  // namespace rm
@@ -212,13 +244,17 @@ int rm_norm_residual(int32_t type, int32_t kind, int32_t rows, int32_t width, co
 
 int rm_trace_begin(rm_launch* records, int32_t capacity)
 {
-    rm::Recording& r = rm::g_recording;
-    if (r.on || capacity < 0 || (capacity > 0 && !records)) return RM_EINVAL;
-    r.records = records;
-    r.capacity = capacity;
-    r.count = 0;
-    r.on = true;
-    return RM_OK;
+    if (rm::g_recording.on || capacity < 0 || (capacity > 0 && !records)) return RM_EINVAL;
+    return rm::begin(records, nullptr, nullptr, capacity);
+}
+
+int rm_trace_begin_timed(rm_launch* records, float* microseconds, int32_t capacity)
+{
+    if (rm::g_recording.on || capacity < 0 || (capacity > 0 && (!records || !microseconds)))
+        return RM_EINVAL;
+    hipEvent_t* events = new (std::nothrow) hipEvent_t[2 * (size_t)capacity + 1]();
+    if (!events) return rm::launch_failed(hipErrorOutOfMemory);
+    return rm::begin(records, microseconds, events, capacity);
 }
 
 int rm_trace_end(int32_t* n_launches)
@@ -226,8 +262,22 @@ int rm_trace_end(int32_t* n_launches)
     rm::Recording& r = rm::g_recording;
     if (!r.on || !n_launches) return RM_EINVAL;
     *n_launches = r.count;
+    hipError_t failed = hipSuccess;
+    for (int64_t i = 0; r.events && i < r.capacity; ++i) {
+        hipEvent_t* at = r.events + 2 * i;
+        if (i < r.count) {
+            float ms = 0.0f;
+            hipError_t e = hipEventSynchronize(at[1]);
+            if (e == hipSuccess) e = hipEventElapsedTime(&ms, at[0], at[1]);
+            if (failed == hipSuccess) failed = e;
+            r.microseconds[i] = ms * 1e3f;
+        }
+        for (int k = 0; k < 2; ++k)
+            if (at[k]) (void)hipEventDestroy(at[k]);
+    }
+    delete[] r.events;
     r = rm::Recording();
-    return RM_OK;
+    return rm::done(failed);
 }
 
 }  // extern "C"

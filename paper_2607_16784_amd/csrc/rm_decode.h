@@ -2,6 +2,7 @@
 // (norm.hip, linear.hip, cache.hip, attend.hip).  Not part of the C ABI.
 #pragma once
 
+#include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 
 #include <cstddef>
@@ -115,6 +116,10 @@ constexpr int kComputeUnits = 256;   // of an MI355X
 // outside a recording.
 void note_launch(const void* kernel, int64_t blocks, unsigned threads, size_t dynamic_lds);
 
+// Events that take the start and end of the next launch on s in a recording
+// with times; null outside one.
+hipError_t launch_events(hipStream_t s, hipEvent_t& begin, hipEvent_t& end);
+
 // A dispatch holds fewer than 2^32 work-items.
 constexpr int64_t most_blocks(unsigned threads) { return 0xffffffffll / threads; }
 
@@ -124,8 +129,12 @@ inline hipError_t launch(void (*kernel)(P...), dim3 grid, unsigned threads, size
                          hipStream_t s, A... args)
 {
     if (grid.x > most_blocks(threads)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, s, args...);
-    const hipError_t e = hipGetLastError();
+    hipEvent_t begin, end;
+    hipError_t e = launch_events(s, begin, end);
+    if (e != hipSuccess) return e;
+    if (begin) hipExtLaunchKernelGGL(kernel, grid, dim3(threads), lds, s, begin, end, 0, args...);
+    else hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, s, args...);
+    e = hipGetLastError();
     if (e == hipSuccess)
         note_launch(reinterpret_cast<const void*>(kernel),
                     (int64_t)grid.x * grid.y * grid.z, threads, lds);

@@ -159,36 +159,27 @@ def trace(model, state, new=1, repeats=16):
     """One step's kernels: a list of dicts name, grid, threads, regs, smem,
     duration (microseconds).
 
-    A call is timed alone, `repeats` of it in a graph; where it is several
-    launches they share its time by their threads."""
-    x = torch.randn((state["table"].shape[0] * new, model.width), device=model.device)
-    x = x.to(model.dtype)
-    state["lengths"] += new
-    kernels = []
-    for name, run in model.calls(x, state, new):
-        with api.rm_trace() as recorded:
-            run()
-        if not recorded.launches:
-            continue
-        side = torch.cuda.Stream()
-        side.wait_stream(torch.cuda.current_stream())
-        graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(graph, stream=side):
-            for _ in range(repeats):
+    The step runs `repeats` times and each launch is timed in its place there, so
+    its weights and its part of the cache come from where a step finds them; its
+    duration is the median."""
+    with torch.cuda.device(model.device):
+        x = torch.randn((state["table"].shape[0] * new, model.width), device=model.device)
+        x = x.to(model.dtype)
+        state["lengths"] += new
+        names = []
+        for name, run in model.calls(x, state, new):
+            with api.rm_trace() as recorded:
                 run()
-        torch.cuda.current_stream().wait_stream(side)
-        begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
-        graph.replay()
-        begin.record()
-        graph.replay()
-        end.record()
-        end.synchronize()
-        took = begin.elapsed_time(end) * 1e3 / repeats
-        run()                                   # the graph's outputs are the graph's
-        threads = sum(k["grid"] * k["threads"] for k in recorded.launches)
-        kernels += [dict(k, name=name, duration=took * k["grid"] * k["threads"] / threads)
-                    for k in recorded.launches]
-    return kernels
+            names += [name] * len(recorded.launches)
+        took = []
+        for _ in range(repeats):
+            with api.rm_trace(len(names), timed=True) as recorded:
+                for _, run in model.calls(x, state, new):
+                    run()
+            took.append([k["duration"] for k in recorded.launches])
+    durations = np.median(np.array(took, np.float64).reshape(repeats, -1), axis=0)
+    return [dict(k, name=name, duration=float(t))
+            for k, name, t in zip(recorded.launches, names, durations)]
 
 
 def trace_library(models, new=1):

@@ -221,3 +221,16 @@ def test_the_largest_numbers_pass(calls):
     f, kw = linear()
     f(**dict(kw, group=(1 << 31) - 32, scales=Tensor((8, 1), BF16), zeros=Tensor((8, 1), U8)))
     assert len(calls) == 3
+
+
+def test_a_recording_with_times_is_refused_without_room_for_them():
+    import ctypes
+    lib, n = api.library(), ctypes.c_int32()
+    records, times = (api.Launch * 2)(), (ctypes.c_float * 2)()
+    for args in ((None, times, 2), (records, None, 2), (records, times, -1)):
+        assert lib.rm_trace_begin_timed(*args) == 1
+    assert lib.rm_trace_begin_timed(records, times, 2) == 0
+    assert lib.rm_trace_begin_timed(records, times, 2) == 1 and lib.rm_trace_begin(records, 2) == 1
+    assert lib.rm_trace_end(ctypes.byref(n)) == 0 and n.value == 0
+    assert lib.rm_trace_begin_timed(None, None, 0) == 0
+    assert lib.rm_trace_end(ctypes.byref(n)) == 0
