@@ -401,8 +401,7 @@ typedef u32x4 Codes __attribute__((aligned(1)));
 // fit, mostly all of them, and between two barriers a wave's loop has loads of
 // codes alone, the next batch in flight during one.
 template <class S>
-__global__ __launch_bounds__(S::THREADS) void linear_kernel(LinearArgs a, int32_t cols,
-                                                            int32_t parts_z)
+__global__ __launch_bounds__(S::THREADS) void linear_kernel(LinearArgs a, int32_t cols)
 {
     typedef typename S::type T;
     typedef typename Vec<T>::x8 V;
@@ -425,15 +424,13 @@ __global__ __launch_bounds__(S::THREADS) void linear_kernel(LinearArgs a, int32_
     Tile<S> tile;
     const T* x0 = static_cast<const T*>(a.x) + m0 * a.x_stride;
     const int batches = a.k / S::BATCH;
-    const int begin = (int)((int64_t)blockIdx.z * batches / parts_z);
-    const int end = (int)((int64_t)(blockIdx.z + 1) * batches / parts_z);
     const int per = cols / S::BATCH;
     const Stage<S> stage(lds, rows, cols);
-    for (int b0 = begin; b0 < end; b0 += per) {
-        const int count = min(per, end - b0), c0 = b0 * S::BATCH, here = count * S::BATCH;
+    for (int b0 = 0; b0 < batches; b0 += per) {
+        const int count = min(per, batches - b0), c0 = b0 * S::BATCH, here = count * S::BATCH;
         const int from = b0 + kp * count / S::KP, upto = b0 + (kp + 1) * count / S::KP;
         const int g0 = group_of(a, c0), groups = group_of(a, c0 + here - 1) + 1 - g0;
-        if (b0 > begin) __syncthreads();
+        if (b0 > 0) __syncthreads();
         // x in stretches of 512 columns of a row, a wave each and 8 in flight; the
         // groups of a row of W, a wave each: neighbours in memory.  The first
         // turn of both and the first codes are on their way together.
@@ -502,8 +499,8 @@ __global__ __launch_bounds__(S::THREADS) void linear_kernel(LinearArgs a, int32_
             }
         }
     }
-    rest<S>(a, tile, rg, m0, rows, batches * S::U + blockIdx.z * S::KP + kp, parts_z * S::KP);
-    finish_tile<S>(a, tile, lds, rg, kp, m0, parts_z);
+    rest<S>(a, tile, rg, m0, rows, batches * S::U + kp, S::KP);
+    finish_tile<S>(a, tile, lds, rg, kp, m0, 1);
 }
 
 // Several tiles of rows of x: the columns go by in chunks of a batch for every
@@ -651,7 +648,7 @@ hipError_t launch_shape(K kernel, size_t lds, const LinearArgs& a, int parts_z, 
                                                  (int)lds);
         if (e != hipSuccess) return e;
     }
-    const hipError_t e = launch(kernel, grid, S::THREADS, lds, s, a, more..., (int32_t)parts_z);
+    const hipError_t e = launch(kernel, grid, S::THREADS, lds, s, a, more...);
     if (e != hipSuccess || parts_z == 1) return e;
     const int64_t threads = (int64_t)out_n * ((a.rows + 3) / 4);
     return launch(linear_join_kernel<typename S::type, S::ACT>,
@@ -659,17 +656,17 @@ hipError_t launch_shape(K kernel, size_t lds, const LinearArgs& a, int parts_z, 
 }
 
 template <typename T, int R, int PER, int ACT, int U, int RG, int KP>
-hipError_t launch_few(const LinearArgs& a, int parts_z, size_t most_lds, hipStream_t s)
+hipError_t launch_few(const LinearArgs& a, size_t most_lds, hipStream_t s)
 {
     typedef Shape<T, R, 1, PER, ACT, U, RG, KP> S;
     const int rows = a.rows < 16 ? a.rows : 16;
-    int cols = (a.k / S::BATCH + parts_z - 1) / parts_z * S::BATCH;
+    int cols = a.k / S::BATCH * S::BATCH;
     auto bytes = [&](int c) { return Stage<S>::bytes(rows, c, c / a.group + 2); };
     if (bytes(cols) > most_lds) {
         cols = S::BATCH * KP;
         while (bytes(cols + S::BATCH * KP) <= most_lds) cols += S::BATCH * KP;
     }
-    return launch_shape<S>(linear_kernel<S>, bytes(cols), a, parts_z, s, (int32_t)cols);
+    return launch_shape<S>(linear_kernel<S>, bytes(cols), a, 1, s, (int32_t)cols);
 }
 
 template <typename T, int R, int M, int PER, int ACT, int U, int RG, int KP, int DEPTH>
@@ -679,7 +676,8 @@ hipError_t launch_many(const LinearArgs& a, int parts_z, hipStream_t s)
     constexpr int COLS = KP * S::BATCH;
     const int rows = a.rows < 16 * M ? a.rows : 16 * M;
     return launch_shape<S>(linear_stream_kernel<S, DEPTH>,
-                           2 * Stage<S>::bytes(rows, COLS, COLS / (32 * PER) + 1), a, parts_z, s);
+                           2 * Stage<S>::bytes(rows, COLS, COLS / (32 * PER) + 1), a, parts_z, s,
+                           (int32_t)parts_z);
 }
 
 // What is taken for which sizes; us at the sizes named, measured one after the
@@ -740,8 +738,8 @@ hipError_t launch_rows(const LinearArgs& a, hipStream_t s)
     constexpr int ONE = ACT == RM_ACT_SWIGLU ? 2 : 1;       // the least tiles a wave
     const Plan p = plan_of(a.rows, a.n, a.k, ACT);
     switch (p.kind) {
-    case kRows: return launch_few<T, ONE, PER, ACT, 2, 1, 8>(a, 1, kMostLds, s);
-    case kRowsWide: return launch_few<T, ONE, PER, ACT, 2, 4, 2>(a, 1, 64 * 1024, s);
+    case kRows: return launch_few<T, ONE, PER, ACT, 2, 1, 8>(a, kMostLds, s);
+    case kRowsWide: return launch_few<T, ONE, PER, ACT, 2, 4, 2>(a, 64 * 1024, s);
     case kTile: return launch_many<T, 2, 1, PER, ACT, 2, 4, 2, 2>(a, p.parts_z, s);
     case kTile2: return launch_many<T, 2, 2, PER, ACT, 1, 4, 2, 2>(a, p.parts_z, s);
     case kTile2Tall: return launch_many<T, 2, 2, PER, ACT, 1, 8, 1, 2>(a, p.parts_z, s);
