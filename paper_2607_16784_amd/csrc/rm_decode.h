@@ -167,13 +167,10 @@ __device__ inline Sequence sequence_of(const rm_sequences& s, int32_t page_token
 // most_blocks they come in several launches.
 constexpr int64_t kMostBlocks = 0x7fffffff;
 
-// New tokens that a sequence of the call can have; 1 at least, so that every
-// sequence has a workgroup that reports one out of range.
-inline int64_t most_tokens(const rm_sequences& s)
-{
-    const int32_t n = s.max_tokens < s.n_tokens ? s.max_tokens : s.n_tokens;
-    return n > 1 ? n : 1;
-}
+// New tokens that a sequence is laid out for; 1 at least, so that every sequence
+// has a workgroup that reports one out of range.  Not bounded by n_tokens: a
+// workspace stays right for calls of fewer tokens.
+inline int64_t most_tokens(const rm_sequences& s) { return s.max_tokens > 1 ? s.max_tokens : 1; }
 
 struct NormArgs {
     int32_t rows, width, gate_width;

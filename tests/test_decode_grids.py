@@ -7,9 +7,15 @@ def test_attention_beyond_31_bits_of_workgroups(lib):  # noqa: F811
     assert lib.rm_cache_attention(0, cache(), s, 4, P, 64, 64, 1.0, 0, P, P, 1 << 60, None,
                                   None) == 3
     assert lib.rm_cache_attention_workspace_bytes(cache(), s, 4) == 0
-    # the bound on a sequence's tokens is that of the call where it is larger
-    s = seqs(n_seqs=65535, max_tokens=1 << 20, n_tokens=1 << 10)
-    assert lib.rm_cache_attention_workspace_bytes(cache(), s, 4) > 0
+
+
+def test_a_workspace_serves_calls_of_fewer_tokens(lib):  # noqa: F811
+    for n, most, stride in ((2, 1, 3), (9, 700, 4000), (3, 64, 100000), (64, 512, 300)):
+        need = {lib.rm_cache_attention_workspace_bytes(
+            cache(kv_heads=4), seqs(n_seqs=n, max_tokens=most, table_stride=stride,
+                                    n_tokens=tokens), 16)
+            for tokens in (1, 7, n, most, n * most)}
+        assert len(need) == 1 and min(need) > 0
 
 
 def test_append_beyond_31_bits_of_workgroups(lib):  # noqa: F811
