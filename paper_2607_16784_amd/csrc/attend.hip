@@ -317,11 +317,11 @@ attend_kernel(AttendArgs a, Plan plan, int64_t first)
         const bool finite = fabsf(v_scale) < INFINITY;
         const float power = finite && v_scale != 0.0f
                                 ? (float)__builtin_amdgcn_frexp_expf(v_scale) : -INFINITY;
-        float top[C], share[C], high[C];
+        float x[C], share[C];
         bool moved = false;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            float x = -INFINITY;
+            x[c] = -INFINITY;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -334,19 +334,20 @@ attend_kernel(AttendArgs a, Plan plan, int64_t first)
                         v = seen ? v : -INFINITY;
                     }
                     sc[i][c][k] = v;
-                    x = fmaxf(x, v);
+                    x[c] = fmaxf(x[c], v);
                 }
-            top[c] = fmaxf(m[c], rows_reduce<Max>(x));
-            high[c] = fmaxf(r[c], rows_reduce<Max>(x + power));
-            moved |= top[c] > m[c] || high[c] > r[c];
+            moved |= x[c] > m[c] || x[c] + power > r[c];
         }
+        // no lane has more than its row's maxima after the first blocks, mostly
         if (__any(moved)) {
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                l[c] *= top[c] == -INFINITY ? 1.0f : exp2_of(m[c] - top[c]);
-                const float shrink = high[c] == -INFINITY ? 1.0f : exp2_of(r[c] - high[c]);
-                m[c] = top[c];
-                r[c] = high[c];
+                const float top = fmaxf(m[c], rows_reduce<Max>(x[c]));
+                const float high = fmaxf(r[c], rows_reduce<Max>(x[c] + power));
+                l[c] *= top == -INFINITY ? 1.0f : exp2_of(m[c] - top);
+                const float shrink = high == -INFINITY ? 1.0f : exp2_of(r[c] - high);
+                m[c] = top;
+                r[c] = high;
 #pragma unroll
                 for (int d = 0; d < D / 16; ++d) o[d][c] *= shrink;
             }
