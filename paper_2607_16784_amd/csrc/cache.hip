@@ -214,14 +214,14 @@ __device__ inline void turn_queries(const AppendArgs& a, int32_t token, int part
 template <typename T, int FMT>
 __global__ __launch_bounds__(1024) void append_kernel(AppendArgs a, int32_t q_blocks,
                                                       int32_t q_parts, int32_t pages_a_seq,
-                                                      int32_t group, int64_t first)
+                                                      int32_t group, uint32_t first)
 {
     __shared__ float2 turn[16][kMostPairs];
     __shared__ float part[16];
-    const int64_t index = first + blockIdx.x;
-    if (index < q_blocks) {
+    const uint32_t index = first + blockIdx.x;      // 31 bits at most (kMostBlocks)
+    if (index < (uint32_t)q_blocks) {
         const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-        const int64_t at = index * waves + wave, token = at / q_parts;
+        const int64_t at = (int64_t)index * waves + wave, token = at / q_parts;
         if (token < a.seqs.n_tokens)
             turn_queries<T>(a, (int32_t)token, (int)(at % q_parts), q_parts, turn[wave]);
         return;
@@ -231,10 +231,10 @@ __global__ __launch_bounds__(1024) void append_kernel(AppendArgs a, int32_t q_bl
     const int TK = a.cache.page_tokens, D = a.cache.head_dim, KV = a.cache.kv_heads;
     const int groups = blockDim.x / group, sides = 2 * KV;
     const int per_page = (sides + groups - 1) / groups;
-    int64_t at = index - q_blocks;
-    const int part_of = (int)(at % per_page);
-    at /= per_page;
-    const int page_no = (int)(at % pages_a_seq), b = (int)(at / pages_a_seq);
+    uint32_t at = index - (uint32_t)q_blocks;
+    const int part_of = (int)(at % (uint32_t)per_page);
+    at /= (uint32_t)per_page;
+    const int page_no = (int)(at % (uint32_t)pages_a_seq), b = (int)(at / (uint32_t)pages_a_seq);
     const Sequence s = sequence_of(a.seqs, TK, b);
     if (s.bad && a.status && threadIdx.x == 0) atomicOr(a.status, RM_ST_BAD_LENGTH);
     const int start = s.length - s.n;                       // first new token
@@ -507,7 +507,7 @@ hipError_t launch_append(int type, const AppendArgs& a, hipStream_t s)
         for (int64_t first = 0; first < p.blocks && e == hipSuccess; first += most)
             e = launch(kernel, dim3((unsigned)(p.blocks - first < most ? p.blocks - first : most)),
                        (unsigned)p.threads, 0, s, a, (int32_t)p.q_blocks, p.q_parts, p.pages,
-                       (int32_t)p.group, first);
+                       (int32_t)p.group, (uint32_t)first);
         return e;
     };
     if (type == RM_TYPE_BF16)
