@@ -473,28 +473,16 @@ def _named(names, value, what):
 
 # ctypes takes the low 32 bits of a larger number without a word.
 
-def _int32(value, name):
-    if -1 << 31 <= value < 1 << 31:
-        return value
-    raise ValueError(f"{name}: {value} does not fit 32 bits")
-
-
-def _sizes_fit(*sizes):
-    if max(sizes) >> 31:
-        raise ValueError(f"sizes beyond 31 bits: {sizes}")
+def _too_large(name, *values):
+    raise ValueError(f"{name}: {values} beyond 31 bits")
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _current_gpu = getattr(torch._C, "_cuda_getDevice", None)
 
 
-def _call(function, gpu, *args):
-    """The entry point on this GPU and its current stream.  The GPU has to be the
-    current one: a default stream's handle is 0 on every GPU."""
-    if _current_gpu() == gpu:
-        return function(*args, _raw_stream(gpu))
-    with torch.cuda.device(gpu):
-        return function(*args, _raw_stream(gpu))
+# A call runs on the current stream of its tensors' GPU, which has to be the current
+# GPU for it: a default stream's handle is 0 on every GPU.
 
 
 def new_cache(n_pages, kv_heads, page_tokens, head_dim, codes=torch.int8, device="cuda"):
@@ -530,11 +518,13 @@ def _sequences_of(table, lengths, token_offsets, n_tokens, max_tokens, gpu):
         raise ValueError("table: expected [sequences, pages]")
     n, pages = shape = table.shape
     if (n | pages | n_tokens) >> 31:
-        _sizes_fit(n, pages, n_tokens)
+        _too_large("sizes", n, pages, n_tokens)
+    if not -1 << 31 <= max_tokens < 1 << 31:
+        _too_large("max_tokens", max_tokens)
     return Sequences(_on_gpu(table, torch.int32, shape, gpu, "table"),
                      _on_gpu(lengths, torch.int32, (n,), gpu, "lengths"),
                      _on_gpu(token_offsets, torch.int32, (n + 1,), gpu, "token_offsets"),
-                     n, pages, n_tokens, _int32(max_tokens, "max_tokens"))
+                     n, pages, n_tokens, max_tokens)
 
 
 def rm_w4_linear(x, codes, scales, group, zeros=None, bias=None, act="none", out=None,
@@ -544,6 +534,9 @@ def rm_w4_linear(x, codes, scales, group, zeros=None, bias=None, act="none", out
     x's type; zeros uint8 like scales (None: 8); bias [n].  act "swiglu" takes
     the first half of the outputs as gates of the second."""
     (kind, gpu), dtype = _type_of(x, "x"), x.dtype
+    if gpu != _current_gpu():
+        with torch.cuda.device(gpu):
+            return rm_w4_linear(x, codes, scales, group, zeros, bias, act, out, workspace)
     if x.dim() != 2 or codes.dim() != 2:
         raise ValueError("rm_w4_linear: expected x [rows, k] and codes [n, ceil(k / 2)]")
     rows, k = shape = x.shape
@@ -551,7 +544,7 @@ def rm_w4_linear(x, codes, scales, group, zeros=None, bias=None, act="none", out
     if group < 1 or group % 32:
         raise ValueError(f"group: expected a multiple of 32, got {group}")
     if (rows | n | k | group) >> 31:
-        _sizes_fit(rows, n, k, group)
+        _too_large("sizes", rows, n, k, group)
     row_bytes = (k + 1) // 2
     groups = (n, -(-k // group))
     act = _named(ACT_NAMES, act, "act")
@@ -568,14 +561,14 @@ def rm_w4_linear(x, codes, scales, group, zeros=None, bias=None, act="none", out
             _on_gpu(scales, dtype, groups, gpu, "scales"),
             _on_gpu(zeros, torch.uint8, groups, gpu, "zeros"),
             _on_gpu(bias, dtype, (n,), gpu, "bias"), act, out.data_ptr(), out_pitch)
-    lib = _lib or library()
+    lib, stream = _lib or library(), _raw_stream(gpu)
     if workspace is None:
-        code = _call(lib.rm_w4_linear, gpu, *args, None, 0)
+        code = lib.rm_w4_linear(*args, None, 0, stream)
         if code == RM_EWORKSPACE:     # most sizes need none, so it is asked for only then
             workspace = torch.empty(lib.rm_w4_linear_workspace_bytes(rows, n, k, act),
                                     dtype=torch.uint8, device=x.device)
     if workspace is not None:
-        code = _call(lib.rm_w4_linear, gpu, *args, *_scratch(workspace, gpu))
+        code = lib.rm_w4_linear(*args, *_scratch(workspace, gpu), stream)
     if code:
         _check(code, "rm_w4_linear")
     return out
@@ -589,6 +582,10 @@ def rm_rotary_append(q, k, v, inv_freq, cache, table, lengths, token_offsets=Non
     already.  q, k and v may be views of one projection.  Returns the turned
     q (None for q None)."""
     (kind, gpu), dtype = _type_of(k, "k"), k.dtype
+    if gpu != _current_gpu():
+        with torch.cuda.device(gpu):
+            return rm_rotary_append(q, k, v, inv_freq, cache, table, lengths, token_offsets,
+                                    max_tokens, positions, layout, rot_scale, q_out, status)
     c = _cache_of(cache, gpu)
     if k.dim() != 3:
         raise ValueError("k: expected [tokens, kv_heads, head_dim]")
@@ -609,13 +606,12 @@ def rm_rotary_append(q, k, v, inv_freq, cache, table, lengths, token_offsets=Non
         else:
             op = _on_gpu(q_out, dtype, shape, gpu, "q_out")
     half = inv_freq.numel()
-    code = _call(
-        (_lib or library()).rm_rotary_append, gpu,
+    code = (_lib or library()).rm_rotary_append(
         kind, c, s, heads, qp, qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0],
         vs[1], _on_gpu(positions, torch.int32, (tokens,), gpu, "positions"),
         _on_gpu(inv_freq, torch.float32, (half,), gpu, "inv_freq"), 2 * half,
         _named(ROTARY_NAMES, layout, "layout"), rot_scale, op,
-        _on_gpu(status, torch.int32, (1,), gpu, "status"))
+        _on_gpu(status, torch.int32, (1,), gpu, "status"), _raw_stream(gpu))
     if code:
         _check(code, "rm_rotary_append")
     return q_out
@@ -627,20 +623,22 @@ def rm_cache_read(cache, pages, dtype=torch.bfloat16, status=None):
     gpu = pages.get_device()
     if gpu < 0:
         raise ValueError(f"pages: expected a GPU tensor, got one on {pages.device}")
+    if gpu != _current_gpu():
+        with torch.cuda.device(gpu):
+            return rm_cache_read(cache, pages, dtype, status)
     c = _cache_of(cache, gpu)
     n = pages.numel()
     if n >> 31:
-        _sizes_fit(n)
+        _too_large("sizes", n)
     kind = TYPES.get(dtype)
     if kind is None:
         raise ValueError(f"dtype: expected bfloat16 or float16, got {dtype}")
     both = torch.empty((2, n, c.page_tokens, c.kv_heads, c.head_dim), dtype=dtype,
                        device=pages.device)
     k, v = both.unbind()
-    code = _call(
-        (_lib or library()).rm_cache_read, gpu,
+    code = (_lib or library()).rm_cache_read(
         kind, c, n, _on_gpu(pages, torch.int32, (n,), gpu, "pages"), k.data_ptr(), v.data_ptr(),
-        _on_gpu(status, torch.int32, (1,), gpu, "status"))
+        _on_gpu(status, torch.int32, (1,), gpu, "status"), _raw_stream(gpu))
     if code:
         _check(code, "rm_cache_read")
     return k, v
@@ -651,6 +649,12 @@ def rm_cache_attention(q, cache, table, lengths, token_offsets=None, max_tokens=
     """Attention of q [tokens, heads, dim] over the cache (causal; `window` > 0
     keeps each token's last `window`).  scale None: 1 / sqrt(dim)."""
     (kind, gpu), dtype = _type_of(q, "q"), q.dtype
+    if gpu != _current_gpu():
+        with torch.cuda.device(gpu):
+            return rm_cache_attention(q, cache, table, lengths, token_offsets, max_tokens, scale,
+                                      window, workspace, out, status)
+    if not -1 << 31 <= window < 1 << 31:
+        _too_large("window", window)
     c = _cache_of(cache, gpu)
     if q.dim() != 3:
         raise ValueError("q: expected [tokens, heads, head_dim]")
@@ -663,16 +667,18 @@ def rm_cache_attention(q, cache, table, lengths, token_offsets=None, max_tokens=
         if need == 0:
             raise ValueError("rm_cache_attention: invalid sizes or options")
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        wp = workspace.data_ptr()
+    else:
+        wp, need = _scratch(workspace, gpu)
     if out is None:
         out = q.new_empty(shape)
         op = out.data_ptr()
     else:
         op = _on_gpu(out, dtype, shape, gpu, "out")
-    code = _call(
-        lib.rm_cache_attention, gpu,
+    code = lib.rm_cache_attention(
         kind, c, s, heads, q.data_ptr(), qs[0], qs[1], dim ** -0.5 if scale is None else scale,
-        _int32(window, "window"), op, *_scratch(workspace, gpu),
-        _on_gpu(status, torch.int32, (1,), gpu, "status"))
+        window, op, wp, need,
+        _on_gpu(status, torch.int32, (1,), gpu, "status"), _raw_stream(gpu))
     if code:
         _check(code, "rm_cache_attention")
     return out
@@ -685,11 +691,15 @@ def rm_norm_residual(x, y=None, gate=None, post_weight=None, pre_weight=None, pr
     x, y [rows, width]; gate [width], [rows, 1] or [rows, width].  Without y
     x' is x itself."""
     (code_type, gpu), dtype = _type_of(x, "x"), x.dtype
+    if gpu != _current_gpu():
+        with torch.cuda.device(gpu):
+            return rm_norm_residual(x, y, gate, post_weight, pre_weight, pre_bias, kind, alpha,
+                                    eps, x_out, n_out)
     if x.dim() != 2:
         raise ValueError("x: expected [rows, width]")
     rows, width = shape = x.shape
     if (rows | width) >> 31:
-        _sizes_fit(rows, width)
+        _too_large("sizes", rows, width)
     x_pitch = _pitch(_rows(x, dtype, shape, gpu, "x")[0], rows, width, "x")
     yp, y_pitch = None, 0
     if y is not None:
@@ -718,12 +728,11 @@ def rm_norm_residual(x, y=None, gate=None, post_weight=None, pre_weight=None, pr
     else:
         no = _on_gpu(n_out, dtype, shape, gpu, "n_out")
     wide = (width,)
-    code = _call(
-        (_lib or library()).rm_norm_residual, gpu,
+    code = (_lib or library()).rm_norm_residual(
         code_type, _named(NORM_NAMES, kind, "kind"), rows, width, x.data_ptr(), x_pitch, yp,
         y_pitch, gp, gs, gw, _on_gpu(post_weight, dtype, wide, gpu, "post_weight"),
         _on_gpu(pre_weight, dtype, wide, gpu, "pre_weight"),
-        _on_gpu(pre_bias, dtype, wide, gpu, "pre_bias"), alpha, eps, xo, no)
+        _on_gpu(pre_bias, dtype, wide, gpu, "pre_bias"), alpha, eps, xo, no, _raw_stream(gpu))
     if code:
         _check(code, "rm_norm_residual")
     return x_out, n_out
