@@ -544,8 +544,8 @@ int rm_w4_linear(int32_t type, int32_t rows, int32_t n, int32_t k, const void* x
  *   (a, b) -> rot_scale * (a cos(p f) - b sin(p f), a sin(p f) + b cos(p f)),
  * f = inv_freq[i] for pair i of `layout`, in the first `rot` channels of each
  * head; the others are copied.  p = positions[token], or the token's index in
- * its sequence where positions is NULL.  The angle is taken modulo one turn
- * in fp64, so that long contexts lose nothing.
+ * its sequence where positions is NULL (0 for a token of no sequence).  The
+ * angle is taken modulo one turn in fp64, so that long contexts lose nothing.
  * q [n_tokens][heads][head_dim], k and v [n_tokens][kv_heads][head_dim]:
  * strides in elements of tokens (q_stride ...) and heads (q_head_stride ...),
  * channels consecutive.  q_out [n_tokens][heads][head_dim].
@@ -588,7 +588,8 @@ int rm_cache_read(int32_t type, const rm_cache* cache, int32_t n, const int32_t*
  * that sees nothing (its sequence or a page is out of range) gets 0, and so do
  * rows that no sequence holds.
  * q as in rm_rotary_append, out [n_tokens][heads][head_dim].  Logits, softmax
- * statistics and sums are fp32; a cached code is exact in the product's type;
+ * statistics and sums are fp32 (sums of q times code, so elements of q up to
+ * 2e33); a cached code is exact in the product's type;
  * the softmax weights enter the second product as f16 numbers, times the scale
  * of the values' page and relative to the row's largest such product so far.
  * Tokens that a row does not see do not reach it, whatever their codes and
@@ -614,7 +615,7 @@ int rm_cache_attention(int32_t type, const rm_cache* cache, const rm_sequences* 
  *   u = y, or norm(y) * post_weight;   x' = x + alpha * gate * u;
  *   n = norm(x') * pre_weight + pre_bias.
  * norm is x / sqrt(mean(x^2) + eps) or (x - mean) / sqrt(variance + eps), in
- * fp32 and of the unrounded x'.  Rows of `width` elements; x, y and gate with
+ * fp32 (squares included: elements up to 1e17) and of the unrounded x'.  Rows of `width` elements; x, y and gate with
  * row strides in elements; gate_stride 0 is one row for all.  gate_width is
  * `width`, or 1 for one gate a row.  Each of y (x' = x then), gate, post_weight
  * (y then enters as it is), pre_weight, pre_bias may be NULL, and so may x_out

@@ -55,7 +55,7 @@ __device__ inline void decode8(uint32_t lo, uint32_t hi, bf16x8& out)
         out = bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
     } else {
         // Else the compiler carries the next block's codes as bytes, a register
-        // each: 83 registers spilt, chunks of prompts in bf16 212 us, 105 so; two
+        // each: 83 registers spilt, chunks of prompts in bf16 took 212 us, 105 so; two
         // sequences of 125 000 tokens 106 and 99.
         asm("" : "+v"(lo), "+v"(hi));
 #pragma unroll

@@ -7,8 +7,10 @@
 // channels in registers: the tile that makes both sides of the page wide, 8
 // consecutive key codes a token and 4 consecutive tokens a value channel.  A
 // page's old codes are read only where a new token raises the scale; the rest
-// of the time a decode step writes its own token's codes alone.  Bound by the
-// traffic of the tokens and of the pages' codes.
+// of the time a decode step writes its own token's codes, and zeros to the slots
+// behind it: what a table or a length that went back had left there is gone.  The
+// zeros are most of what such a step writes (pages of 128: 63 slots on average).
+// Bound by the traffic of the tokens and of the pages' codes.
 //
 // Angles: position * inv_freq in fp64, the whole turns taken off, then sine and
 // cosine in fp32; at position 1e6 an fp32 product would be off by up to 0.03.
@@ -31,7 +33,9 @@ __device__ inline double turns_of(const float* inv_freq, int pair)
 // of the last turn goes through v_sin_f32 and v_cos_f32, which take turns: off
 // by up to 1.3e-7 over [-1/2, 1/2] (measured), against 5e-8 of sincospif, whose
 // instructions bound the prompts' append (7600 tokens, the same again and again:
-// 47.5 us, 40.3 so, 35.2 without any angle; 52 with inputs that change).
+// 47.5 us, 40.3 so, 35.2 without any angle; 51 with inputs that change).  That is
+// 2^-23 of a turn's largest value where the results keep 11 bits, and sines of
+// small angles are right to those 11 bits too.
 __device__ inline void turn_of(double turns, int32_t position, float scale, float& cs, float& sn)
 {
     const double a = (double)position * turns;

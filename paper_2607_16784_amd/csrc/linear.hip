@@ -5,7 +5,8 @@
 // bound by reading the codes once, so everything serves that: the codes are
 // read as they are, row by row, 16 bytes a lane, and expanded in registers.
 //
-// Expansion: two codes sit 4 nibbles apart in a word, so (w >> 4s) & 0x000f000f
+// Expansion, by the usual exact conversion of small integers through a fixed
+// exponent (Kim et al. 2022): two codes sit 4 nibbles apart in a word, so (w >> 4s) & 0x000f000f
 // is the pair (s, s+4) in the low bits of two 16-bit numbers, and OR-ing an
 // exponent makes it (128 + code) * 2^-15 (bf16) or 1024 + code (f16), exactly.  x is
 // put into the same order 0 4 1 5 2 6 3 7.  f16 then subtracts 1024 + zero (exact).
@@ -712,7 +713,8 @@ Plan plan_of(int32_t rows, int32_t n, int32_t k, int act)
         p.kind = kTile2;
         blocks = (tiles + (act == RM_ACT_SWIGLU ? 3 : 7)) / (act == RM_ACT_SWIGLU ? 4 : 8);
     } else {
-        // 64 x 8192 x 28672: 69 us in eight parts, 80 in sixteen
+        // 64 x 8192 x 28672: 78 us in eight parts, 90 in sixteen (here and below in a
+        // graph whose calls alternate between two sets of weights)
         blocks = (tiles + (act == RM_ACT_SWIGLU ? 7 : 15)) / (act == RM_ACT_SWIGLU ? 8 : 16) *
                  ((rows + 63) / 64);
     }
@@ -725,8 +727,8 @@ Plan plan_of(int32_t rows, int32_t n, int32_t k, int act)
     // 64 x 2048 x 28672: 34.6 us in sixteen parts, 51.2 in eight
     if (p.parts_z > 16) p.parts_z = 16;
     if (p.parts_z < 1) p.parts_z = 1;
-    // 64 rows of x a workgroup where that fills the CUs (64 x 8192 x 28672: 81 us
-    // in a graph, 32 rows 97), else 32 (64 x 4096 x 14336 in groups of 32: 44 us, 64
+    // 64 rows of x a workgroup where that fills the CUs (64 x 8192 x 28672: 78 us,
+    // 32 rows 99), else 32 (64 x 4096 x 14336 in groups of 32: 44 us, 64
     // rows 80; 48 x 6000 x 5000: 29 and 35; 128 x 4096 x 4096: 21 and 27)
     if (p.kind == kTile4 && blocks * p.parts_z < kComputeUnits) p.kind = kTile2Tall;
     return p;

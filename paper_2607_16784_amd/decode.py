@@ -21,9 +21,10 @@ from . import api
 def rotary_frequencies(rot, base=10000.0, scaling="none", factor=1.0, trained=4096):
     """(inv_freq float32 [rot / 2], rot_scale) of rm_rotary_append.
 
-    scaling "linear" divides positions by `factor`; "ntk" raises the base so that
-    the slowest pair turns `factor` times slower and the fastest as before;
-    "parts" divides the pairs that turn fewer than once over `trained` positions,
+    The angles are those of Su et al. 2021.  scaling "linear" divides positions by
+    `factor` (Chen et al. 2023); "ntk" raises the base so that the slowest pair
+    turns `factor` times slower and the fastest as before; "parts" (Peng et al.
+    2023) divides the pairs that turn fewer than once over `trained` positions,
     keeps those that turn more than 32 times and goes linearly between, with
     queries and keys scaled up by 0.1 ln(factor) + 1 each."""
     i = np.arange(0, rot, 2, dtype=np.float64) / rot
