@@ -57,3 +57,29 @@ def test_all_around_the_turn():
                 # near a zero the turn, rounded to fp32, is off by 2^-25 of half a turn
                 tol = (2.0 ** -11 + 2.0 ** -20) * abs(want) + 2.0 ** -22
                 assert abs(float(got[t, i]) / 2048.0 - want) <= tol, (p, i)
+
+
+def test_a_million_angles_round_as_the_exact_ones():
+    # f16 results are the exact value's neighbour, but where that is within what
+    # fp32 may be off of the middle between two: the angle's rounding in turns, up
+    # to 2^-26 of one (9.4e-8), and half a last place of the value (3e-8)
+    tokens, dim = 4096, 256
+    g = torch.Generator().manual_seed(7)
+    inv = (torch.rand(dim // 2, generator=g) * 3.1).float()
+    positions = torch.randint(0, 5000, (tokens,), generator=g, dtype=torch.int32)
+    q = torch.zeros((tokens, 1, dim), dtype=torch.float16, device="cuda")
+    q[..., :dim // 2] = 1.0
+    cache = api.new_cache(tokens // 128, 1, 128, dim)
+    k = torch.zeros((tokens, 1, dim), dtype=torch.float16, device="cuda")
+    pages = torch.arange(tokens // 128, dtype=torch.int32, device="cuda")
+    out = api.rm_rotary_append(
+        q, k, k, inv.cuda(), cache, pages[None],
+        torch.tensor([tokens], dtype=torch.int32, device="cuda"), max_tokens=tokens,
+        token_offsets=torch.tensor([0, tokens], dtype=torch.int32, device="cuda"),
+        positions=positions.cuda())[:, 0].double().cpu()
+    angle = positions.double()[:, None] * inv.double()
+    for got, want in ((out[:, :dim // 2], torch.cos(angle)), (out[:, dim // 2:], torch.sin(angle))):
+        # half a unit in the last place of f16 at the value, 2^-25 where it is subnormal
+        half = torch.exp2(torch.floor(torch.log2(want.abs().clamp(min=2.0 ** -14))) - 11)
+        off = (got - want).abs() - half
+        assert float(off.max()) <= 1.2e-7, float(off.max())
