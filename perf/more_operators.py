@@ -1,0 +1,388 @@
+"""Timed cases of the operators of a prompt, with their inputs, their minimal
+work, their plain form in elementary torch operations (32 bits, rounded once)
+and their definition in 64 bits.
+
+The operators are what a served model adds for its prompts, and for weights of
+8 bits, to the decode layer: attention over packed whole prompts, norms of each
+head's queries and keys with the rotation behind them, and projections in 8-bit
+floating point with a scale for each block of 128.
+
+Packed prompts lie behind each other in the rows of the token arrays; `offsets`
+[sequences + 1] int32 names their borders, and rows behind the last one are
+padding, whose results are 0.  Queries, keys and values are views of one fused
+projection's rows.
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import torch
+
+own = False
+
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16}
+E4M3 = torch.float8_e4m3fn
+EPS = 1e-6
+BLOCK = 128
+ROT_SCALE = 1.1
+
+
+def listed():
+    return [
+        # one short prompt: latency
+        dict(name="prompt-one-short", op="attend", seqs=1, len_min=97, len_max=97, ragged=1,
+             pad=0, heads=32, kv_heads=8, dim=128, window=0, type="bf16"),
+        # the prompts that a server has collected, an empty one among them, and padding rows
+        dict(name="prompt-batch-16", op="attend", seqs=16, len_min=0, len_max=1500, ragged=2,
+             pad=13, heads=32, kv_heads=8, dim=128, window=0, type="bf16"),
+        # documents through a layer that looks at the last thousand tokens; groups of five heads
+        dict(name="prompt-window", op="attend", seqs=4, len_min=2500, len_max=5001, ragged=3,
+             pad=0, heads=20, kv_heads=4, dim=64, window=1000, type="f16"),
+        # one long document
+        dict(name="prompt-long", op="attend", seqs=1, len_min=16384, len_max=16384, ragged=4,
+             pad=0, heads=32, kv_heads=8, dim=128, window=0, type="bf16"),
+        # one new token between the projection and the cache
+        dict(name="headnorm-one-token", op="headnorm", tokens=1, heads=32, kv_heads=8, dim=128,
+             rot=128, layout="half", far=131072, weights=True, type="bf16"),
+        # a batch of requests, part of an uncommon head turned, channels in neighbouring pairs
+        dict(name="headnorm-batch-odd", op="headnorm", tokens=61, heads=20, kv_heads=4, dim=80,
+             rot=36, layout="interleaved", far=8192, weights=False, type="f16"),
+        # the tokens of a long prompt
+        dict(name="headnorm-prompt", op="headnorm", tokens=8190, heads=32, kv_heads=8, dim=128,
+             rot=128, layout="half", far=8192, weights=True, type="bf16"),
+        # one token through a square projection of width 4096
+        dict(name="f8-one-token", op="f8", rows=1, n=4096, k=4096, given=False, bias=False,
+             act="none", type="bf16"),
+        # a few requests; outputs and columns that fill no block
+        dict(name="f8-few-odd", op="f8", rows=5, n=1021, k=5150, given=False, bias=True,
+             act="none", type="f16"),
+        # the gate and up projections of a batch of 64, activation included
+        dict(name="f8-gated-64", op="f8", rows=64, n=28672, k=4096, given=False, bias=False,
+             act="swiglu", type="bf16"),
+        # a chunk of prompts whose codes are there already, through a down projection
+        dict(name="f8-given-1000", op="f8", rows=1000, n=2048, k=5632, given=True, bias=False,
+             act="none", type="bf16"),
+        # a large batch of prompts through a wide projection
+        dict(name="f8-prompts", op="f8", rows=8192, n=8192, k=8192, given=False, bias=False,
+             act="none", type="bf16"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi + 0.5)))))))
+
+
+def _any(rng, op):
+    kind = rng.choice(["bf16", "f16"])
+    if op == "f8":
+        act = rng.choice(["none", "none", "swiglu"])
+        n, k = _log(rng, 64, 28672), _log(rng, 64, 28672)
+        k = k if rng.random() < 0.25 else -(-k // 16) * 16 if rng.random() < 0.3 else -(-k // BLOCK) * BLOCK
+        return dict(op=op, rows=_log(rng, 1, 8192), n=n + n % 2, k=k, given=rng.random() < 0.25,
+                    bias=rng.random() < 0.3, act=act, type=kind)
+    kv = rng.choice([1, 2, 4, 8])
+    heads = kv * rng.choice([1, 2, 4, 5, 8] if kv > 1 else [4, 8, 16])
+    if op == "headnorm":
+        dim = rng.choice([64, 72, 80, 96, 128, 128, 192, 256])
+        rot = rng.choice([dim, dim, dim // 2, dim // 4])
+        return dict(op=op, tokens=_log(rng, 1, 8192), heads=heads, kv_heads=kv, dim=dim, rot=rot,
+                    layout=rng.choice(["half", "interleaved"]), far=_log(rng, 64, 1 << 20),
+                    weights=rng.random() < 0.7, type=kind)
+    top = _log(rng, 1, 16384)
+    return dict(op=op, seqs=_log(rng, 1, 64), len_min=rng.choice([0, top // 2, top]), len_max=top,
+                ragged=rng.randrange(1 << 20), pad=rng.choice([0, 0, 1, 70]), heads=heads,
+                kv_heads=kv, dim=rng.choice([64, 128, 128, 256]),
+                window=rng.choice([0, 0, 0, _log(rng, 1, 4096)]), type=kind)
+
+
+def _padded(case):
+    """Logits of the plain form, whose sequences are padded to the longest."""
+    return case["seqs"] * case["heads"] * case["len_max"] ** 2 if case["op"] == "attend" else 0
+
+
+def draw(rng):
+    op = rng.choice(["attend", "attend", "headnorm", "f8", "f8"])
+    ours = [c for c in listed() if c["op"] == op]
+    most = {u: max(work(c)[u] for c in ours) for u in ("bytes", "flops")}
+    logits = max(_padded(c) for c in ours)
+    while True:
+        case = _any(rng, op)
+        w = work(case)
+        if all(w[u] <= most[u] for u in most) and _padded(case) <= logits:
+            return case
+
+
+def _lengths(case):
+    rng = random.Random(case["ragged"])
+    n = [rng.randint(case["len_min"], case["len_max"]) for _ in range(case["seqs"])]
+    n[0] = max(1, n[0])
+    if case["len_min"] == 0 and case["seqs"] > 1:
+        n[case["seqs"] // 2] = 0         # one sequence that brings nothing
+    return n
+
+
+def _pairs(n, window):
+    """Pairs (row, token that it sees) of one sequence."""
+    w = min(n, window) if window else n
+    return w * (w + 1) // 2 + (n - w) * w
+
+
+def _scale_rows(case):
+    """Blocks of 128 rows of the weights; the halves of a gated projection have their own."""
+    if case["act"] == "swiglu":
+        return 2 * (-(-(case["n"] // 2) // BLOCK))
+    return -(-case["n"] // BLOCK)
+
+
+def work(case):
+    c = case
+    if c["op"] == "f8":
+        m, n, k, blocks = c["rows"], c["n"], c["k"], -(-c["k"] // BLOCK)
+        out = n // 2 if c["act"] == "swiglu" else n
+        size = (n * k + 4 * _scale_rows(c) * blocks + m * (k + 4 * blocks if c["given"] else 2 * k) +
+                2 * m * out + (2 * n if c["bias"] else 0))
+        return {"bytes": size, "flops": 2 * m * n * k}
+    if c["op"] == "headnorm":
+        both = c["tokens"] * (c["heads"] + c["kv_heads"])
+        size = 4 * both * c["dim"] + 4 * c["tokens"] + 2 * c["rot"]
+        size += 4 * c["dim"] if c["weights"] else 0
+        return {"bytes": size, "flops": both * (4 * c["dim"] + 3 * c["rot"])}
+    n = _lengths(c)
+    tokens = sum(n)
+    size = tokens * (2 * c["heads"] + 2 * c["kv_heads"]) * c["dim"] * 2 + 4 * (len(n) + 1)
+    size += c["pad"] * c["heads"] * c["dim"] * 2
+    return {"bytes": size,
+            "flops": 4 * c["heads"] * c["dim"] * sum(_pairs(x, c["window"]) for x in n)}
+
+
+# --------------------------------------------------------------------------- inputs
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    c, dt = case, TYPES[case["type"]]
+
+    def normal(*shape):
+        return torch.randn(shape, generator=gen, device="cuda")
+
+    st = {"case": c}
+    if c["op"] == "f8":
+        n, k = c["n"], c["k"]
+        rows, blocks = _scale_rows(c), -(-k // BLOCK)
+        w = normal(n, k).div_(math.sqrt(k))
+        half = n // 2 if c["act"] == "swiglu" else n
+        st["block"] = torch.arange(n, device="cuda")        # of each row
+        st["block"] = st["block"] % half // BLOCK + st["block"] // half * (rows // (n // half))
+        # a block's scale is its largest value / 448, as weights are laid out offline
+        top = torch.zeros((rows, blocks), device="cuda")
+        wide = torch.zeros((n, blocks * BLOCK), device="cuda")
+        wide[:, :k] = w
+        peak = wide.view(n, blocks, BLOCK).abs().amax(dim=2)
+        top.scatter_reduce_(0, st["block"][:, None].expand(n, blocks), peak, "amax")
+        st["scales"] = top.clamp(min=1e-20) / 448.0
+        wide.view(n, blocks, BLOCK).div_(st["scales"][st["block"]][:, :, None])
+        st["codes"] = wide[:, :k].clamp(-448, 448).to(E4M3)
+        # channels of different size, as activations have them
+        x = normal(c["rows"], k) * torch.exp(0.7 * normal(k))
+        if c["given"]:
+            wide = torch.zeros((c["rows"], blocks * BLOCK), device="cuda")
+            wide[:, :k] = x
+            wide = wide.view(-1, blocks, BLOCK)
+            st["x_scales"] = wide.abs().amax(dim=2).clamp(min=1e-20) / 448.0
+            wide.div_(st["x_scales"][:, :, None])
+            st["x"] = wide.view(c["rows"], -1)[:, :k].clamp(-448, 448).to(E4M3)
+        else:
+            st["x_scales"], st["x"] = None, x.to(dt)
+        st["bias"] = normal(n).to(dt) if c["bias"] else None
+        return st
+    h, kv, d = c["heads"], c["kv_heads"], c["dim"]
+    if c["op"] == "headnorm":
+        rows = c["tokens"]
+        st["inv_freq"] = torch.tensor([10000.0 ** (-2.0 * i / c["rot"])
+                                       for i in range(c["rot"] // 2)],
+                                      dtype=torch.float32, device="cuda")
+        st["positions"] = torch.randint(0, c["far"], (rows,), generator=gen, device="cuda",
+                                        dtype=torch.int32)
+        st["q_weight"], st["k_weight"] = (((1 + normal(d) / 8).to(dt) for _ in range(2))
+                                          if c["weights"] else (None, None))
+        # heads and tokens of different size, which the norm takes out
+        qkv = normal(rows, h + 2 * kv, d) * torch.exp(normal(rows, h + 2 * kv, 1))
+    else:
+        offsets = [0]
+        for n in _lengths(c):
+            offsets.append(offsets[-1] + n)
+        rows = offsets[-1] + c["pad"]
+        st["offsets"] = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+        st["most"] = max(b - a for a, b in zip(offsets, offsets[1:]))
+        qkv = normal(rows, h + 2 * kv, d)
+        # some heads look at few tokens, others at many
+        qkv[:, :h] *= torch.exp(0.5 * normal(h, 1))
+    qkv = qkv.to(dt)
+    st["q"], st["k"], st["v"] = qkv[:, :h], qkv[:, h:h + kv], qkv[:, h + kv:]
+    return st
+
+
+# --------------------------------------------------------------------------- one pass
+
+def run(state):
+    return (_kernels if own else _plain)(state)
+
+
+def _kernels(s):
+    from paper_2607_16784_amd import api
+    c = s["case"]
+    if c["op"] == "f8":
+        return api.rm_f8_linear(s["x"], s["codes"], s["scales"], x_scales=s["x_scales"],
+                                bias=s["bias"], act=c["act"], dtype=TYPES[c["type"]])
+    if c["op"] == "headnorm":
+        q, k = api.rm_head_norm_rotary(s["q"], s["k"], s["inv_freq"], s["positions"],
+                                       q_weight=s["q_weight"], k_weight=s["k_weight"],
+                                       layout=c["layout"], rot_scale=ROT_SCALE, eps=EPS)
+        return {"q": q, "k": k}
+    return api.rm_prompt_attention(s["q"], s["k"], s["v"], s["offsets"], s["most"],
+                                   window=c["window"])
+
+
+def _plain(s):
+    return {"f8": _plain_f8, "headnorm": _plain_headnorm, "attend": _plain_attend}[s["case"]["op"]](s)
+
+
+def _plain_f8(s):
+    c, k = s["case"], s["case"]["k"]
+    blocks = -(-k // BLOCK)
+    if c["given"]:
+        x = s["x"].float() * s["x_scales"].repeat_interleave(BLOCK, dim=1)[:, :k]
+    else:
+        x = torch.zeros((c["rows"], blocks * BLOCK), device="cuda")
+        x[:, :k] = s["x"]
+        x = x.view(-1, blocks, BLOCK)
+        part, power = torch.frexp(x.abs().amax(dim=2, keepdim=True) / 448.0)
+        power = torch.where(part > 0.5, power, power - 1).clamp(min=-126)
+        x = torch.ldexp(x, -power).to(E4M3).float()
+        x = torch.ldexp(x, power).view(c["rows"], -1)[:, :k]
+    w = s["codes"].float() * s["scales"][s["block"]].repeat_interleave(BLOCK, dim=1)[:, :k]
+    t = x @ w.t()
+    if s["bias"] is not None:
+        t = t + s["bias"].float()
+    if c["act"] == "swiglu":
+        a, b = t.chunk(2, dim=1)
+        t = a / (1 + torch.exp(-a)) * b
+    return t.to(TYPES[c["type"]])
+
+
+def _plain_headnorm(s):
+    c, rot = s["case"], s["case"]["rot"]
+    turn = s["positions"].double()[:, None] * s["inv_freq"].double()
+    turn = torch.remainder(turn, 2 * math.pi).float()[:, None]
+    cos, sin = torch.cos(turn) * ROT_SCALE, torch.sin(turn) * ROT_SCALE
+
+    def one(x, weight):
+        x = x.float()
+        x = x * torch.rsqrt((x * x).mean(dim=2, keepdim=True) + EPS)
+        x = x if weight is None else x * weight.float()
+        if c["layout"] == "half":
+            u, w = x[..., :rot // 2], x[..., rot // 2:rot]
+            turned = torch.cat((u * cos - w * sin, u * sin + w * cos), dim=-1)
+        else:
+            u, w = x[..., 0:rot:2], x[..., 1:rot:2]
+            turned = torch.stack((u * cos - w * sin, u * sin + w * cos), dim=-1).flatten(-2)
+        return torch.cat((turned, x[..., rot:]), dim=-1).to(TYPES[c["type"]])
+
+    return {"q": one(s["q"], s["q_weight"]), "k": one(s["k"], s["k_weight"])}
+
+
+def _plain_attend(s):
+    c, off = s["case"], s["offsets"].long()
+    seqs, most, kv, d = c["seqs"], s["most"], c["kv_heads"], c["dim"]
+    per = c["heads"] // kv
+    tokens = s["q"].shape[0] - c["pad"]
+    at = torch.arange(tokens, device="cuda")
+    seq = torch.searchsorted(off[1:], at, right=True)
+    i = at - off[seq]
+
+    def padded(x):
+        full = torch.zeros((seqs, most) + x.shape[1:], device="cuda")
+        full[seq, i] = x[:tokens].float()
+        return full
+
+    q = padded(s["q"]).view(seqs, most, kv, per, d).permute(0, 2, 3, 1, 4)
+    k = padded(s["k"]).permute(0, 2, 3, 1).reshape(seqs * kv, d, most)
+    v = padded(s["v"]).transpose(1, 2).reshape(seqs * kv, most, d)
+    p = torch.bmm(q.reshape(seqs * kv, per * most, d) / math.sqrt(d), k)
+    col = torch.arange(most, device="cuda")
+    row = col[:, None]
+    hidden = col > row
+    if c["window"]:
+        hidden |= col <= row - c["window"]
+    # every row sees itself at least, so none is without a largest logit
+    p = p.view(seqs * kv, per, most, most).masked_fill_(hidden, -math.inf)
+    p.sub_(p.amax(dim=-1, keepdim=True)).exp_()
+    total = p.sum(dim=-1).view(seqs * kv, per * most, 1)
+    o = torch.bmm(p.view(seqs * kv, per * most, most), v) / total
+    o = o.view(seqs, kv, per, most, d).permute(0, 3, 1, 2, 4).reshape(seqs, most, -1, d)
+    out = torch.zeros(s["q"].shape, dtype=s["q"].dtype, device="cuda")
+    out[:tokens] = o[seq, i].to(out.dtype)
+    return out
+
+
+# --------------------------------------------------------------------------- 64 bits
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return {"f8": _exact_f8, "headnorm": _exact_headnorm, "attend": _exact_attend}[case["op"]](s)
+
+
+def _exact_f8(s):
+    c, k = s["case"], s["case"]["k"]
+    t = torch.zeros((c["rows"], c["n"]), dtype=torch.float64, device="cuda")
+    for b, lo in enumerate(range(0, k, BLOCK)):
+        x = s["x"][:, lo:lo + BLOCK].double()
+        if c["given"]:
+            x = x * s["x_scales"][:, b:b + 1].double()
+        else:
+            # the smallest power of two that holds the block's largest value within 448
+            top = x.abs().amax(dim=1, keepdim=True)
+            scale = torch.exp2(torch.log2(top / 448).ceil().clamp(min=-126))
+            scale = torch.where(top > 448 * scale, scale * 2, scale)
+            scale = torch.where(top <= 224 * scale, scale / 2, scale).clamp(min=2.0 ** -126)
+            x = (x / scale).float().to(E4M3).double() * scale
+        w = s["codes"][:, lo:lo + BLOCK].double()
+        t += x @ w.t() * s["scales"][:, b].double()[s["block"]]
+    if s["bias"] is not None:
+        t += s["bias"].double()
+    if c["act"] == "swiglu":
+        half = c["n"] // 2
+        t = t[:, :half] * torch.sigmoid(t[:, :half]) * t[:, half:]
+    return t
+
+
+def _exact_headnorm(s):
+    c, rot = s["case"], s["case"]["rot"]
+    turn = torch.polar(torch.tensor(ROT_SCALE, dtype=torch.float64, device="cuda"),
+                       s["positions"].double()[:, None] * s["inv_freq"].double())[:, None]
+    first, second = ((slice(0, rot // 2), slice(rot // 2, rot)) if c["layout"] == "half"
+                     else (slice(0, rot, 2), slice(1, rot, 2)))
+    out = {}
+    for name in ("q", "k"):
+        x = s[name].double()
+        x = x / (x.square().sum(2, keepdim=True) / c["dim"] + EPS).sqrt()
+        if s[name + "_weight"] is not None:
+            x = x * s[name + "_weight"].double()
+        z = torch.complex(x[..., first].contiguous(), x[..., second].contiguous()) * turn
+        x[..., first], x[..., second] = z.real, z.imag
+        out[name] = x
+    return out
+
+
+def _exact_attend(s):
+    c, off = s["case"], s["offsets"].tolist()
+    per = c["heads"] // c["kv_heads"]
+    out = torch.zeros(s["q"].shape, dtype=torch.float64, device="cuda")
+    for lo, hi in zip(off, off[1:]):
+        j = torch.arange(hi - lo, device="cuda")
+        hidden = (j > j[:, None]) | (j <= j[:, None] - (c["window"] or hi - lo + 1))
+        for h in range(c["heads"] if hi > lo else 0):
+            k, v = (s[n][lo:hi, h // per].double() for n in ("k", "v"))
+            p = s["q"][lo:hi, h].double() @ k.t() / c["dim"] ** 0.5
+            out[lo:hi, h] = p.masked_fill_(hidden, -math.inf).softmax(dim=1) @ v
+    return out
