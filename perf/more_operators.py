@@ -258,8 +258,8 @@ def _plain_f8(s):
         x = x.view(-1, blocks, BLOCK)
         part, power = torch.frexp(x.abs().amax(dim=2, keepdim=True) / 448.0)
         power = torch.where(part > 0.5, power, power - 1).clamp(min=-126)
-        x = torch.ldexp(x, -power).to(E4M3).float()
-        x = torch.ldexp(x, power).view(c["rows"], -1)[:, :k]
+        scale = ((power + 127) << 23).view(torch.float32)      # 2^power to the last bit
+        x = ((x / scale).to(E4M3).float() * scale).view(c["rows"], -1)[:, :k]
     w = s["codes"].float() * s["scales"][s["block"]].repeat_interleave(BLOCK, dim=1)[:, :k]
     t = x @ w.t()
     if s["bias"] is not None:
