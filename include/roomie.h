@@ -19,6 +19,10 @@
  *   rm_cache_read            the values that pages of the cache hold
  *   rm_cache_attention       attention over the cache
  *   rm_norm_residual         gated, scaled residual between two norms
+ *   rm_head_norm_rotary      norms of each head's queries and keys, rotated
+ *   rm_prompt_attention      attention over packed whole prompts
+ *   rm_f8_quantize           8-bit floating codes with a scale for each block
+ *   rm_f8_linear             projection in 8-bit floating point
  *   rm_trace_begin, _end     the launch shapes of these calls, as rm_occupancy
  *                            takes them, and their times
  *
@@ -124,7 +128,11 @@ extern "C" {
 #define RM_MAX_W4_COLUMNS  2097152  /* k of rm_w4_linear                       */
 #define RM_MAX_W4_OUTPUTS 536870848 /* n of rm_w4_linear                       */
 #define RM_MAX_W4_ROWS     4194240  /* rows of rm_w4_linear                    */
-#define RM_MAX_SEQUENCES     65535  /* n_seqs of the cache calls               */
+#define RM_MAX_SEQUENCES     65535  /* n_seqs of the cache calls and prompts   */
+#define RM_MAX_HEAD_WIDTH      512  /* head_dim of rm_head_norm_rotary         */
+#define RM_MAX_F8_COLUMNS  2097152  /* k of rm_f8_linear and rm_f8_quantize    */
+#define RM_MAX_F8_OUTPUTS 536870848 /* n of rm_f8_linear                       */
+#define RM_MAX_F8_ROWS     4194240  /* rows of rm_f8_linear                    */
 
 /* Target-device descriptor: the SM limits of Eq. (1) and Eq. (2).
  * W = max_threads_per_sm / warp_size must be an integer <= 127, and the four
@@ -630,6 +638,101 @@ int rm_norm_residual(int32_t type, int32_t kind, int32_t rows, int32_t width, co
                      const void* pre_weight, const void* pre_bias, float alpha, float eps,
                      void* x_out, void* n_out, void* stream);
 
+/*
+ * rm_head_norm_rotary -- each head's queries and keys normalised and turned by
+ * their positions, one pass:
+ *   u = x / sqrt(mean(x^2) + eps) * weight   over a head's channels,
+ *   (a, b) -> rot_scale * (a cos(p f) - b sin(p f), a sin(p f) + b cos(p f))
+ * of u, with the pairs, frequencies and exact angles of rm_rotary_append and
+ * p = positions[token]; channels from `rot` on are u as it is.  Statistics and
+ * products are fp32 (squares included: elements up to 1e17), each result is
+ * rounded once.  q, q_out [n_tokens][heads][head_dim], k, k_out
+ * [n_tokens][kv_heads][head_dim]: strides in elements of tokens and heads,
+ * channels consecutive.  An output may be its input (same address and strides),
+ * and may otherwise overlap nothing.  q_weight, k_weight [head_dim] or NULL (1).
+ * heads or kv_heads may be 0 (that side is then not read).
+ * Errors: RM_EINVAL (NULL pointer, negative size, rot odd or > head_dim, eps or
+ *   rot_scale not finite, bad type or layout), RM_EUNSUPPORTED (head_dim not a
+ *   multiple of 8 or over RM_MAX_HEAD_WIDTH, heads or kv_heads over 65535),
+ *   RM_ELAUNCH.
+ */
+int rm_head_norm_rotary(int32_t type, int32_t n_tokens, int32_t heads, int32_t kv_heads,
+                        int32_t head_dim, const void* q, int64_t q_stride, int64_t q_head_stride,
+                        const void* k, int64_t k_stride, int64_t k_head_stride,
+                        const void* q_weight, const void* k_weight, const int32_t* positions,
+                        const float* inv_freq, int32_t rot, int32_t layout, float rot_scale,
+                        float eps, void* q_out, int64_t q_out_stride, int64_t q_out_head_stride,
+                        void* k_out, int64_t k_out_stride, int64_t k_out_head_stride,
+                        void* stream);
+
+/*
+ * rm_prompt_attention -- causal attention of packed whole prompts over their own
+ * keys and values.  Sequence b is rows token_offsets[b] .. token_offsets[b+1]-1 of
+ * q [n_tokens][heads][head_dim], k and v [n_tokens][kv_heads][head_dim] and out:
+ *   out[t][h] = sum_j w_j v_j,  w = softmax over j of scale * q[t][h].k_j
+ * of kv head h / (heads / kv_heads), over the rows j of t's sequence with j <= t
+ * and, where window > 0, j > t - window.  Rows of no sequence get 0.
+ * Strides in elements of tokens and heads, channels consecutive; out is dense.
+ * head_dim 64, 128 or 256.  Logits, softmax statistics and sums are fp32; the
+ * softmax weights enter the second product in q's type, relative to a logit no
+ * more than 2^6 below the row's largest so far.  A row that t does not see does
+ * not reach it, whatever its keys and values hold.
+ * token_offsets may not decrease; where they do RM_ST_BAD_LENGTH is set and rows
+ * of out are unspecified.  A sequence of more than max_tokens rows, or one that
+ * leaves [0, n_tokens), sets RM_ST_BAD_LENGTH too, and its rows get 0.
+ * Errors: RM_EINVAL (NULL pointer, negative size, heads not a multiple of
+ *   kv_heads, scale not finite, window < 0, bad type), RM_EUNSUPPORTED (head_dim
+ *   not listed, n_seqs over RM_MAX_SEQUENCES, heads over 65535, max_tokens *
+ *   heads / kv_heads or the workgroups beyond 31 bits), RM_ELAUNCH.
+ */
+int rm_prompt_attention(int32_t type, int32_t n_tokens, int32_t heads, int32_t kv_heads,
+                        int32_t head_dim, const void* q, int64_t q_stride, int64_t q_head_stride,
+                        const void* k, int64_t k_stride, int64_t k_head_stride, const void* v,
+                        int64_t v_stride, int64_t v_head_stride, const int32_t* token_offsets,
+                        int32_t n_seqs, int32_t max_tokens, float scale, int32_t window,
+                        void* out, int32_t* status, void* stream);
+
+/*
+ * rm_f8_quantize -- rows of k elements as e4m3 codes with a scale for each block
+ * of block_rows (1 or 128) rows and 128 columns:
+ *   scale = the smallest power of two, 2^-126 at least, for which the block's
+ *   largest magnitude is at most 448 scale;  code = x / scale, to nearest even.
+ * x / scale is exact, so a code is one rounding.  A block that holds a value
+ * that is not finite gets the scale NaN.  codes: rows of k bytes, code_stride
+ * apart; scales fp32 [ceil(rows / block_rows)][ceil(k / 128)].
+ * Errors: RM_EINVAL (NULL pointer, rows < 0, k < 1, a stride below its row, bad
+ *   type or block_rows), RM_EUNSUPPORTED (k > RM_MAX_F8_COLUMNS), RM_ELAUNCH.
+ */
+int rm_f8_quantize(int32_t type, int32_t rows, int32_t k, const void* x, int64_t x_stride,
+                   int32_t block_rows, uint8_t* codes, int64_t code_stride, float* scales,
+                   void* stream);
+
+/*
+ * rm_f8_linear -- projection in 8-bit floating point, a scale for each block of
+ * 128 columns, for one to many rows:
+ *   t[m][j] = bias[j] + sum over blocks c of x_scales[m][c] * scales[j/128][c] *
+ *             sum over i in c of x[m][i] * code[j][i]
+ *   y = t, or with RM_ACT_SWIGLU y[m][j] = silu(t[m][j]) * t[m][j + n/2].
+ * x: rows of k elements, x_stride apart; of `type`, with x_scales NULL (the call
+ *   takes the codes that rm_f8_quantize makes of them with block_rows 1), or e4m3
+ *   codes with x_scales fp32 [rows][ceil(k/128)].  codes: e4m3, row j at codes +
+ *   j*code_stride; scales fp32 [ceil(n/128)][ceil(k/128)].  With SWIGLU each half
+ *   of the rows has blocks of its own: scales [2 * ceil(n/2/128)][ceil(k/128)].
+ *   bias [n] of `type` or NULL.  y: rows of n (SWIGLU: n/2) elements of `type`,
+ *   y_stride apart.  Sums are fp32, each output is rounded once; scales whose
+ *   product leaves fp32's range give what that product gives.
+ * workspace: rm_f8_linear_workspace_bytes bytes, 256-byte aligned (0 bytes: none,
+ *   workspace may be NULL).  The order of every sum is fixed.
+ * Errors: RM_EINVAL (NULL pointer, rows < 0, n or k < 1, a stride below its row,
+ *   SWIGLU with odd n, bad type or act), RM_EUNSUPPORTED (k > RM_MAX_F8_COLUMNS,
+ *   n > RM_MAX_F8_OUTPUTS, rows > RM_MAX_F8_ROWS), RM_EWORKSPACE, RM_ELAUNCH.
+ */
+size_t rm_f8_linear_workspace_bytes(int32_t rows, int32_t n, int32_t k, int32_t act);
+int rm_f8_linear(int32_t type, int32_t rows, int32_t n, int32_t k, const void* x,
+                 int64_t x_stride, const float* x_scales, const uint8_t* codes,
+                 int64_t code_stride, const float* scales, const void* bias, int32_t act, void* y,
+                 int64_t y_stride, void* workspace, size_t workspace_bytes, void* stream);
+
 /* One launch as the predictor describes a kernel: blocks in the grid, threads
  * a block, vector registers a thread, LDS bytes a block. */
 typedef struct {
@@ -638,9 +741,10 @@ typedef struct {
 
 /*
  * rm_trace_begin / rm_trace_end -- between them every launch of the calling
- * thread's rm_w4_linear, rm_rotary_append, rm_cache_read, rm_cache_attention
- * and rm_norm_residual calls is written to records[0..capacity) (host memory)
- * in order; the launches themselves are as always.  rm_trace_end stores the
+ * thread's rm_w4_linear, rm_rotary_append, rm_cache_read, rm_cache_attention,
+ * rm_norm_residual, rm_head_norm_rotary, rm_prompt_attention, rm_f8_quantize and
+ * rm_f8_linear calls is written to records[0..capacity) (host memory) in order;
+ * the launches themselves are as always.  rm_trace_end stores the
  * number of launches, which may exceed the capacity, and ends the recording.
  * rm_trace_begin_timed -- the same with the time that each launch takes on the
  * device, from its first to its last work-item: rm_trace_end waits for the

@@ -132,12 +132,23 @@ def library():
         lib.rm_cache_attention.argtypes = [i32, C, S, i32, P, i64, i64, f32, i32, P, P, sz, P, P]
         lib.rm_norm_residual.argtypes = [i32, i32, i32, i32, P, i64, P, i64, P, i64, i32, P, P, P,
                                          f32, f32, P, P, P]
+        lib.rm_head_norm_rotary.argtypes = [i32, i32, i32, i32, i32, P, i64, i64, P, i64, i64, P,
+                                            P, P, P, i32, i32, f32, f32, P, i64, i64, P, i64, i64,
+                                            P]
+        lib.rm_prompt_attention.argtypes = [i32, i32, i32, i32, i32, P, i64, i64, P, i64, i64, P,
+                                            i64, i64, P, i32, i32, f32, i32, P, P, P]
+        lib.rm_f8_quantize.argtypes = [i32, i32, i32, P, i64, i32, P, i64, P, P]
+        lib.rm_f8_linear_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        lib.rm_f8_linear_workspace_bytes.restype = sz
+        lib.rm_f8_linear.argtypes = [i32, i32, i32, i32, P, i64, P, P, i64, P, P, i32, P, i64, P,
+                                     sz, P]
         lib.rm_trace_begin.argtypes = [ctypes.POINTER(Launch), i32]
         lib.rm_trace_begin_timed.argtypes = [ctypes.POINTER(Launch), ctypes.POINTER(f32), i32]
         lib.rm_trace_end.argtypes = [ctypes.POINTER(i32)]
         for f in (lib.rm_w4_linear, lib.rm_rotary_append, lib.rm_cache_read,
-                  lib.rm_cache_attention, lib.rm_norm_residual, lib.rm_trace_begin,
-                  lib.rm_trace_begin_timed, lib.rm_trace_end):
+                  lib.rm_cache_attention, lib.rm_norm_residual, lib.rm_head_norm_rotary,
+                  lib.rm_prompt_attention, lib.rm_f8_quantize, lib.rm_f8_linear,
+                  lib.rm_trace_begin, lib.rm_trace_begin_timed, lib.rm_trace_end):
             f.restype = ctypes.c_int
         lib.rm_status_string.argtypes = [ctypes.c_int]
         lib.rm_status_string.restype = ctypes.c_char_p
@@ -455,6 +466,17 @@ def _pitch(stride, rows, width, name):
     return stride
 
 
+def _apart(strides, shape, name):
+    """Strides of an output [tokens, heads, dim] whose rows may not overlap."""
+    (t, h, d), (ts, hs, _) = shape, strides
+    if (h <= 1 or hs >= d) and (t <= 1 or ts >= (h - 1) * hs * (h > 1) + d):
+        return strides
+    # heads in front of the tokens
+    if t > 1 and ts >= d and (h <= 1 or hs >= (t - 1) * ts + d):
+        return strides
+    raise ValueError(f"{name}: rows overlap")
+
+
 def _type_of(t, name):
     """The type's code and the GPU that all tensors of the call have to be on."""
     code, gpu = TYPES.get(t.dtype), t.get_device()
@@ -736,6 +758,184 @@ def rm_norm_residual(x, y=None, gate=None, post_weight=None, pre_weight=None, pr
     if code:
         _check(code, "rm_norm_residual")
     return x_out, n_out
+
+
+def rm_head_norm_rotary(q, k, inv_freq, positions=None, q_weight=None, k_weight=None,
+                        layout="half", rot_scale=1.0, eps=1e-6, q_out=None, k_out=None):
+    """(q, k), each head normalised (times q_weight or k_weight [head_dim]) and
+    turned by its token's position: q [tokens, heads, dim], k [tokens, kv_heads,
+    dim], positions int32 [tokens], 2 * len(inv_freq) channels of each head turn,
+    times rot_scale.  q and k may be views of one projection and may be their own
+    outputs; either may be None."""
+    first = k if q is None else q
+    if first is None:
+        raise ValueError("rm_head_norm_rotary: expected q or k")
+    (kind, gpu), dtype = _type_of(first, "k" if q is None else "q"), first.dtype
+    if gpu != _current_gpu():
+        with torch.cuda.device(gpu):
+            return rm_head_norm_rotary(q, k, inv_freq, positions, q_weight, k_weight, layout,
+                                       rot_scale, eps, q_out, k_out)
+    if first.dim() != 3:
+        raise ValueError("rm_head_norm_rotary: expected q and k [tokens, heads, head_dim]")
+    tokens, _, dim = first.shape
+    heads = kv_heads = 0
+    qp = kp = qo = ko = None
+    qs = ks = qos = kos = (0, 0)
+    if q is not None:
+        heads = q.shape[1]
+        qs, qp = _rows(q, dtype, q.shape, gpu, "q"), q.data_ptr()
+        q_out = q.new_empty(q.shape) if q_out is None else q_out
+        qos, qo = _apart(_rows(q_out, dtype, q.shape, gpu, "q_out"), q.shape, "q_out"), \
+            q_out.data_ptr()
+    if k is not None:
+        if k.dim() != 3:
+            raise ValueError("k: expected [tokens, kv_heads, head_dim]")
+        kv_heads = k.shape[1]
+        shape = (tokens, kv_heads, dim)
+        ks, kp = _rows(k, dtype, shape, gpu, "k"), k.data_ptr()
+        k_out = k.new_empty(shape) if k_out is None else k_out
+        kos, ko = _apart(_rows(k_out, dtype, shape, gpu, "k_out"), shape, "k_out"), \
+            k_out.data_ptr()
+    if (tokens | heads | kv_heads | dim) >> 31:
+        _too_large("sizes", tokens, heads, kv_heads, dim)
+    half = inv_freq.numel()
+    if half >> 30:
+        _too_large("inv_freq", half)
+    wide = (dim,)
+    code = (_lib or library()).rm_head_norm_rotary(
+        kind, tokens, heads, kv_heads, dim, qp, qs[0], qs[1], kp, ks[0], ks[1],
+        _on_gpu(q_weight, dtype, wide, gpu, "q_weight"),
+        _on_gpu(k_weight, dtype, wide, gpu, "k_weight"),
+        _on_gpu(positions, torch.int32, (tokens,), gpu, "positions"),
+        _on_gpu(inv_freq, torch.float32, (half,), gpu, "inv_freq"), 2 * half,
+        _named(ROTARY_NAMES, layout, "layout"), rot_scale, eps, qo, qos[0], qos[1], ko, kos[0],
+        kos[1], _raw_stream(gpu))
+    if code:
+        _check(code, "rm_head_norm_rotary")
+    return q_out, k_out
+
+
+def rm_prompt_attention(q, k, v, token_offsets, max_tokens, scale=None, window=0, out=None,
+                        status=None):
+    """Causal attention of packed whole prompts: q [tokens, heads, dim], k and v
+    [tokens, kv_heads, dim], sequence b in rows token_offsets[b] to
+    token_offsets[b + 1] (int32), none longer than max_tokens; `window` > 0 keeps
+    each token's last `window`.  scale None: 1 / sqrt(dim).  Rows of no sequence
+    get 0."""
+    (kind, gpu), dtype = _type_of(q, "q"), q.dtype
+    if gpu != _current_gpu():
+        with torch.cuda.device(gpu):
+            return rm_prompt_attention(q, k, v, token_offsets, max_tokens, scale, window, out,
+                                       status)
+    if q.dim() != 3 or k.dim() != 3 or token_offsets.dim() != 1 or token_offsets.shape[0] < 1:
+        raise ValueError("rm_prompt_attention: expected q [tokens, heads, head_dim], k and v "
+                         "[tokens, kv_heads, head_dim] and token_offsets [sequences + 1]")
+    tokens, heads, dim = shape = q.shape
+    kv_heads, n = k.shape[1], token_offsets.shape[0] - 1
+    if (tokens | heads | kv_heads | dim | n) >> 31:
+        _too_large("sizes", tokens, heads, kv_heads, dim, n)
+    if not -1 << 31 <= max_tokens < 1 << 31:
+        _too_large("max_tokens", max_tokens)
+    if not -1 << 31 <= window < 1 << 31:
+        _too_large("window", window)
+    kv = (tokens, kv_heads, dim)
+    qs, ks = _rows(q, dtype, shape, gpu, "q"), _rows(k, dtype, kv, gpu, "k")
+    vs = _rows(v, dtype, kv, gpu, "v")
+    if out is None:
+        out = q.new_empty(shape)
+        op = out.data_ptr()
+    else:
+        op = _on_gpu(out, dtype, shape, gpu, "out")
+    code = (_lib or library()).rm_prompt_attention(
+        kind, tokens, heads, kv_heads, dim, q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1],
+        v.data_ptr(), vs[0], vs[1],
+        _on_gpu(token_offsets, torch.int32, (n + 1,), gpu, "token_offsets"), n, max_tokens,
+        dim ** -0.5 if scale is None else scale, window, op,
+        _on_gpu(status, torch.int32, (1,), gpu, "status"), _raw_stream(gpu))
+    if code:
+        _check(code, "rm_prompt_attention")
+    return out
+
+
+def rm_f8_quantize(x, block_rows=1):
+    """(codes, scales) of x [rows, k]: codes float8_e4m3fn [rows, k] and float32
+    scales, powers of two, [ceil(rows / block_rows), ceil(k / 128)], one for each
+    block of block_rows (1 or 128) rows and 128 columns."""
+    (kind, gpu), dtype = _type_of(x, "x"), x.dtype
+    if gpu != _current_gpu():
+        with torch.cuda.device(gpu):
+            return rm_f8_quantize(x, block_rows)
+    if x.dim() != 2:
+        raise ValueError("x: expected [rows, k]")
+    rows, k = shape = x.shape
+    if block_rows not in (1, 128):
+        raise ValueError(f"block_rows: expected 1 or 128, got {block_rows}")
+    if (rows | k) >> 31:
+        _too_large("sizes", rows, k)
+    pitch = _pitch(_rows(x, dtype, shape, gpu, "x")[0], rows, k, "x")
+    codes = x.new_empty(shape, dtype=torch.float8_e4m3fn)
+    scales = x.new_empty((-(-rows // block_rows), -(-k // 128)), dtype=torch.float32)
+    code = (_lib or library()).rm_f8_quantize(kind, rows, k, x.data_ptr(), pitch, block_rows,
+                                              codes.data_ptr(), k, scales.data_ptr(),
+                                              _raw_stream(gpu))
+    if code:
+        _check(code, "rm_f8_quantize")
+    return codes, scales
+
+
+def rm_f8_linear(x, codes, scales, x_scales=None, bias=None, act="none", dtype=None, out=None,
+                 workspace=None):
+    """x [rows, k] through 8-bit floating weights: codes float8_e4m3fn [n, k] (rows
+    may be strided), scales float32 [ceil(n / 128), ceil(k / 128)].  x is bfloat16
+    or float16, quantised by the call for each row and 128 columns, or
+    float8_e4m3fn with x_scales float32 [rows, ceil(k / 128)]; the result is of x's
+    type, or of `dtype` (bfloat16 if None) for codes.  act "swiglu" takes the first
+    half of the outputs as gates of the second, and each half has blocks of its
+    own: scales [2 * ceil(n / 2 / 128), ceil(k / 128)].  bias [n] is of the
+    result's type."""
+    given = x_scales is not None
+    x_type = torch.float8_e4m3fn if given else x.dtype
+    if dtype is None:
+        dtype = out.dtype if out is not None else torch.bfloat16 if given else x_type
+    kind, gpu = TYPES.get(dtype), x.get_device()
+    if kind is None or gpu < 0 or not (given or x_type is dtype):
+        raise ValueError("x: expected a GPU tensor of the result's type, bfloat16 or float16, or "
+                         f"codes with x_scales, got {x.dtype} on {x.device} for {dtype}")
+    if gpu != _current_gpu():
+        with torch.cuda.device(gpu):
+            return rm_f8_linear(x, codes, scales, x_scales, bias, act, dtype, out, workspace)
+    if x.dim() != 2 or codes.dim() != 2:
+        raise ValueError("rm_f8_linear: expected x [rows, k] and codes [n, k]")
+    rows, k = shape = x.shape
+    n = codes.shape[0]
+    if (rows | n | k) >> 31:
+        _too_large("sizes", rows, n, k)
+    act = _named(ACT_NAMES, act, "act")
+    width = n // 2 if act else n
+    blocks = -(-k // 128)
+    bands = 2 * -(-width // 128) if act else -(-n // 128)
+    if out is None:
+        out = x.new_empty((rows, width), dtype=dtype)
+        out_pitch = width
+    else:
+        out_pitch = _pitch(_rows(out, dtype, (rows, width), gpu, "out")[0], rows, width, "out")
+    x_pitch = _pitch(_rows(x, x_type, shape, gpu, "x")[0], rows, k, "x")
+    code_pitch = _pitch(_rows(codes, torch.float8_e4m3fn, (n, k), gpu, "codes")[0], n, k, "codes")
+    args = (kind, rows, n, k, x.data_ptr(), x_pitch,
+            _on_gpu(x_scales, torch.float32, (rows, blocks), gpu, "x_scales"), codes.data_ptr(),
+            code_pitch, _on_gpu(scales, torch.float32, (bands, blocks), gpu, "scales"),
+            _on_gpu(bias, dtype, (n,), gpu, "bias"), act, out.data_ptr(), out_pitch)
+    lib, stream = _lib or library(), _raw_stream(gpu)
+    if workspace is None:
+        code = lib.rm_f8_linear(*args, None, 0, stream)
+        if code == RM_EWORKSPACE:     # few rows need none, so it is asked for only then
+            workspace = torch.empty(lib.rm_f8_linear_workspace_bytes(rows, n, k, act),
+                                    dtype=torch.uint8, device=x.device)
+    if workspace is not None:
+        code = lib.rm_f8_linear(*args, *_scratch(workspace, gpu), stream)
+    if code:
+        _check(code, "rm_f8_linear")
+    return out
 
 
 class rm_trace:

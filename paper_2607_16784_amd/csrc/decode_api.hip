@@ -242,6 +242,98 @@ int rm_norm_residual(int32_t type, int32_t kind, int32_t rows, int32_t width, co
     return rm::done(rm::launch_norm(type, kind, a, (hipStream_t)stream));
 }
 
+int rm_head_norm_rotary(int32_t type, int32_t n_tokens, int32_t heads, int32_t kv_heads,
+                        int32_t head_dim, const void* q, int64_t q_stride, int64_t q_head_stride,
+                        const void* k, int64_t k_stride, int64_t k_head_stride,
+                        const void* q_weight, const void* k_weight, const int32_t* positions,
+                        const float* inv_freq, int32_t rot, int32_t layout, float rot_scale,
+                        float eps, void* q_out, int64_t q_out_stride, int64_t q_out_head_stride,
+                        void* k_out, int64_t k_out_stride, int64_t k_out_head_stride,
+                        void* stream)
+{
+    if (!rm::type_ok(type) || n_tokens < 0 || heads < 0 || kv_heads < 0 || head_dim < 1 ||
+        rot < 0 || rot % 2 || rot > head_dim)
+        return RM_EINVAL;
+    if (layout != RM_ROTARY_HALF && layout != RM_ROTARY_INTERLEAVED) return RM_EINVAL;
+    if (!std::isfinite(rot_scale) || !std::isfinite(eps)) return RM_EINVAL;
+    if (head_dim % 8 || head_dim > RM_MAX_HEAD_WIDTH || heads > 65535 || kv_heads > 65535)
+        return RM_EUNSUPPORTED;
+    if (n_tokens == 0 || (heads == 0 && kv_heads == 0)) return RM_OK;
+    if ((heads > 0 && (!q || !q_out)) || (kv_heads > 0 && (!k || !k_out))) return RM_EINVAL;
+    if (rot > 0 && (!positions || !inv_freq)) return RM_EINVAL;
+    rm::HeadNormArgs a = {n_tokens, heads, kv_heads, head_dim, rot, layout, q, k, q_stride,
+                          q_head_stride, k_stride, k_head_stride, q_weight, k_weight, positions,
+                          inv_freq, rot_scale, eps, q_out, k_out, q_out_stride, q_out_head_stride,
+                          k_out_stride, k_out_head_stride};
+    return rm::done(rm::launch_head_norm(type, a, (hipStream_t)stream));
+}
+
+int rm_prompt_attention(int32_t type, int32_t n_tokens, int32_t heads, int32_t kv_heads,
+                        int32_t head_dim, const void* q, int64_t q_stride, int64_t q_head_stride,
+                        const void* k, int64_t k_stride, int64_t k_head_stride, const void* v,
+                        int64_t v_stride, int64_t v_head_stride, const int32_t* token_offsets,
+                        int32_t n_seqs, int32_t max_tokens, float scale, int32_t window,
+                        void* out, int32_t* status, void* stream)
+{
+    if (!rm::type_ok(type) || n_tokens < 0 || n_seqs < 0 || max_tokens < 0 || kv_heads < 1 ||
+        heads < 1 || heads % kv_heads || window < 0 || !std::isfinite(scale))
+        return RM_EINVAL;
+    if (head_dim != 64 && head_dim != 128 && head_dim != 256) return RM_EUNSUPPORTED;
+    if (n_seqs > RM_MAX_SEQUENCES || heads > 65535) return RM_EUNSUPPORTED;
+    if ((int64_t)max_tokens * (heads / kv_heads) > 0x7fffff00) return RM_EUNSUPPORTED;
+    rm::PromptArgs a = {n_tokens, heads, kv_heads, n_seqs, max_tokens, window, q, k, v, q_stride,
+                        q_head_stride, k_stride, k_head_stride, v_stride, v_head_stride,
+                        token_offsets, scale, out, status};
+    if (!rm::prompt_fits(a)) return RM_EUNSUPPORTED;
+    if (n_tokens == 0) return RM_OK;
+    if (!q || !k || !v || !out || !token_offsets) return RM_EINVAL;
+    return rm::done(rm::launch_prompt(type, head_dim, a, (hipStream_t)stream));
+}
+
+int rm_f8_quantize(int32_t type, int32_t rows, int32_t k, const void* x, int64_t x_stride,
+                   int32_t block_rows, uint8_t* codes, int64_t code_stride, float* scales,
+                   void* stream)
+{
+    if (!rm::type_ok(type) || rows < 0 || k < 1 || x_stride < k || code_stride < k ||
+        (block_rows != 1 && block_rows != 128))
+        return RM_EINVAL;
+    if (k > RM_MAX_F8_COLUMNS) return RM_EUNSUPPORTED;
+    if (rows == 0) return RM_OK;
+    if (!x || !codes || !scales) return RM_EINVAL;
+    rm::QuantizeArgs a = {rows, k, x, x_stride, codes, code_stride, scales};
+    return rm::done(rm::launch_quantize(type, block_rows, a, (hipStream_t)stream));
+}
+
+size_t rm_f8_linear_workspace_bytes(int32_t rows, int32_t n, int32_t k, int32_t act)
+{
+    if (rows < 1 || n < 1 || k < 1 || k > RM_MAX_F8_COLUMNS || n > RM_MAX_F8_OUTPUTS ||
+        rows > RM_MAX_F8_ROWS)
+        return 0;
+    return rm::f8_workspace(rows, n, k, act);
+}
+
+int rm_f8_linear(int32_t type, int32_t rows, int32_t n, int32_t k, const void* x,
+                 int64_t x_stride, const float* x_scales, const uint8_t* codes,
+                 int64_t code_stride, const float* scales, const void* bias, int32_t act, void* y,
+                 int64_t y_stride, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!rm::type_ok(type) || rows < 0 || n < 1 || k < 1) return RM_EINVAL;
+    if (act != RM_ACT_NONE && act != RM_ACT_SWIGLU) return RM_EINVAL;
+    if (act == RM_ACT_SWIGLU && n % 2) return RM_EINVAL;
+    if (x_stride < k || code_stride < k || y_stride < (act == RM_ACT_SWIGLU ? n / 2 : n))
+        return RM_EINVAL;
+    if (k > RM_MAX_F8_COLUMNS || n > RM_MAX_F8_OUTPUTS || rows > RM_MAX_F8_ROWS)
+        return RM_EUNSUPPORTED;
+    if (rows == 0) return RM_OK;
+    if (!x || !codes || !scales || !y) return RM_EINVAL;
+    const size_t need = rm::f8_workspace(rows, n, k, act);
+    if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255)))
+        return RM_EWORKSPACE;
+    rm::F8Args a = {rows, n, k, act, x, x_stride, x_scales, codes, code_stride, scales, bias, y,
+                    y_stride, workspace};
+    return rm::done(rm::launch_f8(type, a, (hipStream_t)stream));
+}
+
 int rm_trace_begin(rm_launch* records, int32_t capacity)
 {
     if (rm::g_recording.on || capacity < 0 || (capacity > 0 && !records)) return RM_EINVAL;

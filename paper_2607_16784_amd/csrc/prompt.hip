@@ -1,0 +1,423 @@
+// prompt.hip -- causal attention of packed whole prompts (rm_prompt_attention).
+//
+// The rows of a tile are 128 (token, query head) pairs that share a kv head,
+// tokens first, 32 a wave.  A workgroup takes 64 keys and values at a time through
+// LDS, with the running maximum and sum of the softmax:
+//   S^T = K Q^T    v_mfma_f32_32x32x16, keys as the 32 rows
+//   O^T += V^T P   the same, value channels as the 32 rows
+// A lane ends up with 32 of the 64 logits of one row, which are, in their order,
+// the operand that the second product wants from it; what it wants of the values,
+// four keys of one channel, is a transposing read of LDS.  Rows never leave their
+// lane, so nothing but maxima and sums passes between lanes, and those between two.
+#include "rm_common.h"
+#include "rm_decode.h"
+
+namespace rm {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kWaves = 4;
+constexpr int kKeys = 64;                // a step
+constexpr int kRows = kWaves * 32;       // (token, head) pairs of a tile
+// Weights are 2^(logit - m) with m at most kSlack below the row's largest logit so
+// far (powers of two): m moves, and the sums with it, only where a logit passes it
+// by more, which after the first keys is seldom.  In f16 a weight of 2^kSlack times
+// 2^9 is within the type, and one of 2^-23 keeps all its bits.
+constexpr float kSlack = 6.0f;
+
+template <typename T> struct Lift;
+template <> struct Lift<bf16> { static constexpr float power = 0.0f; };
+template <> struct Lift<f16> { static constexpr float power = 9.0f; };
+// the bits of the exponent, all of them set where a number is not finite
+template <typename T> struct Exponent;
+template <> struct Exponent<bf16> { static constexpr uint32_t bits = 0x7f80; };
+template <> struct Exponent<f16> { static constexpr uint32_t bits = 0x7c00; };
+
+__device__ inline f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ inline f32x16 mfma(f16x8 a, f16x8 b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// The two lanes of a row, 32 apart.
+template <class Op>
+__device__ inline float halves(float v)
+{
+    const uint32_t b = __builtin_bit_cast(uint32_t, v);
+    const auto h = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    const uint32_t h0 = h[0], h1 = h[1];
+    return Op::of(__builtin_bit_cast(float, h0), __builtin_bit_cast(float, h1));
+}
+
+// Tiles of the sequences lie in a row of slots, sequence b's from
+// floor(first row * group / kRows) + b on: that leaves each enough, whatever the
+// lengths, and the sequence of a slot is found by 64 lanes that ask at once.
+__device__ inline int32_t row_of(const PromptArgs& a, int32_t offset)
+{
+    return min(max(offset, 0), a.n_tokens);
+}
+__device__ inline int64_t first_slot(const PromptArgs& a, int group, int32_t offset, int b)
+{
+    return (int64_t)row_of(a, offset) * group / kRows + b;
+}
+
+// The last sequence whose first slot is at most `slot`, -1 for none.
+__device__ inline int sequence_at(const PromptArgs& a, int group, int64_t slot)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = a.n_seqs;
+    while (true) {
+        const int step = (n + 63) / 64, b = lo + lane * step;
+        const bool before = lane * step < n &&
+                            first_slot(a, group, a.offsets[min(b, a.n_seqs - 1)], b) <= slot;
+        const int hit = __popcll(__ballot(before)) - 1;
+        if (hit < 0) return -1;
+        lo += hit * step;
+        n = min(step, n - hit * step);
+        if (step == 1) return __builtin_amdgcn_readfirstlane(lo);
+    }
+}
+
+// Zeros for rows [lo, hi) of out.
+template <typename T, int D>
+__device__ inline void clear(const PromptArgs& a, int64_t lo, int64_t hi)
+{
+    const int64_t row = (int64_t)a.heads * D;
+    T* out = static_cast<T*>(a.out);
+    for (int64_t i = lo * row + threadIdx.x * 8; i < hi * row; i += kWaves * 64 * 8)
+        store8(out + i, typename Vec<T>::x8{});
+}
+
+// Rows that are in front of the first sequence or behind the last, and the check of
+// the offsets.
+constexpr int kClear = 128;      // rows a workgroup
+
+template <typename T, int D>
+__device__ inline void clear_rows(const PromptArgs& a, int64_t group)
+{
+    const int64_t lo = group * kClear, hi = min(lo + kClear, (int64_t)a.n_tokens);
+    const int64_t begin = a.n_seqs ? a.offsets[0] : a.n_tokens;
+    const int64_t end = a.n_seqs ? a.offsets[a.n_seqs] : a.n_tokens;
+    if (begin > lo) clear<T, D>(a, lo, min(hi, begin));
+    if (end < hi) clear<T, D>(a, max(lo, max(begin, end)), hi);
+    if (group || !a.status) return;
+    bool bad = false;
+    for (int b = threadIdx.x; b < a.n_seqs; b += kWaves * 64) {
+        const int64_t from = a.offsets[b], n = a.offsets[b + 1] - from;
+        bad = bad || from < 0 || n < 0 || n > a.max_tokens || from + n > a.n_tokens;
+    }
+    if (bad) atomicOr(a.status, RM_ST_BAD_LENGTH);
+}
+
+// A step's keys and values in LDS: rows of D channels, chunks of 16 bytes swapped
+// within a row so that the rows an access takes at once are spread over the banks:
+// eight keys, or four of the values.
+template <int D>
+__device__ inline int key_at(int row, int chunk)
+{
+    return row * D + (chunk ^ (row & 7)) * 8;
+}
+template <int D>
+__device__ inline int value_at(int row, int chunk)
+{
+    return row * D + (chunk ^ (row & 3) * 2) * 8;
+}
+
+// The operand of channels 32 d .. and the keys 16 t + 4 h + {0 .. 3, 8 .. 11} of the
+// lane's half h, in the order of the weights.
+template <typename T, int D>
+__device__ inline typename Vec<T>::x8 values_of(const T* values, int d, int t)
+{
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    const int lane = threadIdx.x & 63;
+    const int row = t * 16 + (lane >> 5) * 4 + (lane & 15) / 4;
+    const int chunk = d * 4 + (lane >> 4 & 1) * 2 + (lane & 3) / 2;
+    auto four = [&](int r) {
+        const T* from = values + value_at<D>(r, chunk) + (lane & 1) * 4;
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4*)from);
+    };
+    const s16x4 x = four(row), y = four(row + 8);
+    return __builtin_bit_cast(typename Vec<T>::x8,
+                              (s16x8){x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]});
+}
+
+// Whether any of the step's values is not finite; each lane of a wave has a part.
+template <typename T, int D>
+__device__ inline bool any_odd(const T* values)
+{
+    constexpr uint32_t top = Exponent<T>::bits;
+    bool odd = false;
+#pragma unroll 4
+    for (int i = 0; i < kKeys * D / 512; ++i) {
+        const u32x4 v = reinterpret_cast<const u32x4*>(values)[i * 64 + (threadIdx.x & 63)];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            odd = odd || (v[j] & top) == top || (v[j] >> 16 & top) == top;
+    }
+    return odd;
+}
+
+struct PromptPlan {
+    int64_t slots, clear, first;
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(kWaves * 64) void prompt_kernel(PromptArgs a, PromptPlan plan)
+{
+    typedef typename Vec<T>::x8 V;
+    typedef typename Vec<T>::x2 V2;
+    constexpr int CHUNKS = D / 8, LOADS = kKeys * CHUNKS / (kWaves * 64);
+    __shared__ __align__(1024) T keys[2][kKeys * D], values[2][kKeys * D];
+
+    const int KV = a.kv_heads, G = a.heads / KV;
+    const int64_t at = plan.first + blockIdx.x;
+    if (at >= plan.slots * KV) {
+        clear_rows<T, D>(a, at - plan.slots * KV);
+        return;
+    }
+    const int64_t slot = (uint64_t)at / (uint32_t)KV;
+    const int head = (int)(at - slot * KV);
+    const int b = sequence_at(a, G, slot);
+    if (b < 0) return;
+    const int32_t begin = a.offsets[b], end = a.offsets[b + 1];
+    const int64_t count = (int64_t)end - begin, at_slot = slot - first_slot(a, G, begin, b);
+    if (begin < 0 || end > a.n_tokens || count < 0 || count > a.max_tokens) {
+        // its rows in range, a part each slot and head
+        const int64_t lo = row_of(a, begin), rows = row_of(a, end) - lo;
+        const int64_t from = (at_slot * KV + head) * kRows / ((int64_t)KV * G);
+        const int64_t upto = ((at_slot * KV + head + 1) * kRows - 1) / ((int64_t)KV * G) + 1;
+        clear<T, D>(a, lo + min(from, rows), lo + min(upto, rows));
+        return;
+    }
+    // the last tiles take the longest, so they come first
+    const int64_t rows = count * G, tile = (rows + kRows - 1) / kRows - 1 - at_slot;
+    if (tile < 0) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int li = lane & 31, h = lane >> 5;
+    const int n = (int)count, r0 = (int)(tile * kRows);
+    const int last_row = (int)min(rows, (tile + 1) * kRows) - 1;
+    const int first_pos = r0 / G, last_pos = last_row / G;
+    const int lo = a.window > 0 ? max(0, first_pos - a.window + 1) / kKeys : 0;
+    const int hi = last_pos / kKeys + 1;
+    // of this wave's rows
+    const int wave_r0 = r0 + wave * 32;
+    const int wave_first = min(wave_r0, last_row) / G;
+    const int wave_last = min(wave_r0 + 31, last_row) / G;
+    const int mine = min(wave_r0 + li, last_row), pos = mine / G;
+    const int64_t q_token = begin + pos;
+    const int q_head = head * G + mine % G;
+
+    const T* k_base = static_cast<const T*>(a.k) + begin * a.k_stride + head * a.k_head;
+    const T* v_base = static_cast<const T*>(a.v) + begin * a.v_stride + head * a.v_head;
+    V kr[LOADS], vr[LOADS];
+    auto load = [&](int step) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int c = i * kWaves * 64 + threadIdx.x;
+            const int64_t token = min(step * kKeys + c / CHUNKS, n - 1);
+            kr[i] = load8(k_base + token * a.k_stride + c % CHUNKS * 8);
+            vr[i] = load8(v_base + token * a.v_stride + c % CHUNKS * 8);
+        }
+    };
+    auto store = [&](int buffer) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int c = i * kWaves * 64 + threadIdx.x, row = c / CHUNKS, chunk = c % CHUNKS;
+            *reinterpret_cast<V*>(&keys[buffer][key_at<D>(row, chunk)]) = kr[i];
+            *reinterpret_cast<V*>(&values[buffer][value_at<D>(row, chunk)]) = vr[i];
+        }
+    };
+
+    V q[D / 16];
+    {
+        const T* row = static_cast<const T*>(a.q) + q_token * a.q_stride + q_head * a.q_head;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            q[i] = load8(row + i * 16 + h * 8);
+            if (a.scale < 0) q[i] = -q[i];
+            if (a.scale == 0) q[i] = q[i] * (T)0.0f;
+        }
+    }
+    // positive, so that the largest logit is that of the largest product, and so that
+    // what is masked stays -infinity
+    const float to_log2 = a.scale == 0 ? 1.0f : fabsf(a.scale) * 1.44269504088896340736f;
+    f32x16 o[D / 32];
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    float m = -INFINITY, l = 0.0f;
+
+    load(lo);
+    for (int step = lo; step < hi; ++step) {
+        const int buffer = step & 1, t0 = step * kKeys;
+        store(buffer);
+        __syncthreads();
+        load(min(step + 1, hi - 1));
+        if (t0 > wave_last || (a.window > 0 && t0 + kKeys <= wave_first - a.window + 1)) continue;
+
+        f32x16 s[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[u][i] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                const V e = *reinterpret_cast<const V*>(
+                    &keys[buffer][key_at<D>(u * 32 + li, i * 2 + h)]);
+                s[u] = mfma(e, q[i], s[u]);
+            }
+        }
+        // of register i of part u: key t0 + 32 u + 8 (i / 4) + 4 h + i % 4
+        const bool masked = t0 + kKeys - 1 > wave_first ||
+                            (a.window > 0 && t0 <= wave_last - a.window);
+        if (masked) {
+            const int upto = pos - t0 - 4 * h, from = a.window > 0 ? upto - a.window : -kKeys - 8;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int j = u * 32 + i / 4 * 8 + i % 4;
+                    if (j > upto || j <= from) s[u][i] = -INFINITY;
+                }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
+        top = halves<Max>(top) * to_log2;
+        if (__any(top > m + kSlack)) {
+            // rows that have seen nothing yet have sums of 0
+            const float to = fmaxf(m, top);
+            const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= f;
+        }
+        const float off = m == -INFINITY ? 0.0f : m - Lift<T>::power;
+        V p[4];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], to_log2, -off));
+                l += e;
+                p[u * 2 + i / 8][i % 8] = (T)e;
+            }
+        const T* tile_v = values[buffer];
+        const bool odd = masked && __any(any_odd<T, D>(tile_v));
+        if (odd) {
+            // 0 times a value that is not finite would reach rows that do not see it:
+            // those that do get it here, and the product is without it
+            for (int j = 0; j < kKeys; ++j) {
+                const int key = t0 + j;
+                if (key > pos || (a.window > 0 && key <= pos - a.window)) continue;
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int c = d * 32 + i / 4 * 8 + h * 4 + i % 4;
+                        const float v = (float)tile_v[value_at<D>(j, c / 8) + c % 8];
+                        if (!(fabsf(v) < INFINITY)) o[d][i] += v;
+                    }
+            }
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    V e = values_of<T, D>(tile_v, d, t);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (!(fabsf((float)e[i]) < INFINITY)) e[i] = (T)0.0f;
+                    o[d] = mfma(e, p[t], o[d]);
+                }
+            continue;
+        }
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) o[d] = mfma(values_of<T, D>(tile_v, d, t), p[t], o[d]);
+    }
+    l = halves<Add>(l);
+    const float inv = 1.0f / l;
+    T* out = static_cast<T*>(a.out) + (q_token * a.heads + q_head) * D;
+    const bool mine_too = wave_r0 + li <= last_row;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            // channels 4 h .. and 8 + 4 h ..: the halves of a row swap to get eight
+            uint32_t w[2][2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int r = (j * 2 + i) * 4 + e * 2;
+                    const V2 two = {(T)(o[d][r] * inv), (T)(o[d][r + 1] * inv)};
+                    w[i][e] = __builtin_bit_cast(uint32_t, two);
+                }
+            const auto x = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
+            const auto y = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+            const uint32_t x0 = x[0], x1 = x[1], y0 = y[0], y1 = y[1];
+            if (mine_too)
+                store8(out + d * 32 + j * 16 + h * 8,
+                       __builtin_bit_cast(V, (u32x4){x0, y0, x1, y1}));
+        }
+}
+
+PromptPlan plan_of(const PromptArgs& a)
+{
+    PromptPlan p;
+    const int64_t group = a.heads / a.kv_heads;
+    p.slots = a.n_seqs ? (int64_t)a.n_tokens * group / kRows + a.n_seqs : 0;
+    p.clear = ((int64_t)a.n_tokens + kClear - 1) / kClear;
+    p.first = 0;
+    return p;
+}
+
+template <typename T, int D>
+hipError_t launch_form(const PromptArgs& a, hipStream_t s)
+{
+    PromptPlan p = plan_of(a);
+    const int64_t all = p.slots * a.kv_heads + p.clear, most = most_blocks(kWaves * 64) / 8 * 8;
+    for (p.first = 0; p.first < all; p.first += most) {
+        const int64_t n = all - p.first < most ? all - p.first : most;
+        const hipError_t e = launch(prompt_kernel<T, D>, dim3((unsigned)n), kWaves * 64, 0, s, a, p);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <typename T>
+hipError_t launch_type(int head_dim, const PromptArgs& a, hipStream_t s)
+{
+    if (head_dim == 64) return launch_form<T, 64>(a, s);
+    if (head_dim == 128) return launch_form<T, 128>(a, s);
+    return launch_form<T, 256>(a, s);
+}
+
+}  // namespace
+
+bool prompt_fits(const PromptArgs& a)
+{
+    const PromptPlan p = plan_of(a);
+    return p.slots * a.kv_heads + p.clear <= 0x7fffffff;
+}
+
+hipError_t launch_prompt(int type, int head_dim, const PromptArgs& a, hipStream_t s)
+{
+    return type == RM_TYPE_BF16 ? launch_type<bf16>(head_dim, a, s)
+                                : launch_type<f16>(head_dim, a, s);
+}
+
+}  // namespace rm

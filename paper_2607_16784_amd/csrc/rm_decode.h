@@ -1,5 +1,5 @@
-// rm_decode.h -- definitions shared by the kernels of a decode layer
-// (norm.hip, linear.hip, cache.hip, attend.hip).  Not part of the C ABI.
+// rm_decode.h -- definitions shared by the kernels of a served model's layer
+// (norm.hip, linear.hip, cache.hip, attend.hip; headnorm.hip, prompt.hip, f8.hip).  Not part of the C ABI.
 #pragma once
 
 #include <hip/hip_ext.h>
@@ -226,5 +226,58 @@ struct AttendArgs {
 bool attend_fits(const rm_cache& c, const rm_sequences& s, int32_t heads);
 size_t attend_workspace(const rm_cache& c, const rm_sequences& s, int32_t heads);
 hipError_t launch_attend(int type, const AttendArgs& a, hipStream_t s);
+
+struct HeadNormArgs {
+    int32_t n_tokens, heads, kv_heads, head_dim, rot, layout;
+    const void *q, *k;
+    int64_t q_stride, q_head, k_stride, k_head;
+    const void *q_weight, *k_weight;
+    const int32_t* positions;
+    const float* inv_freq;
+    float rot_scale, eps;
+    void *q_out, *k_out;
+    int64_t q_out_stride, q_out_head, k_out_stride, k_out_head;
+};
+hipError_t launch_head_norm(int type, const HeadNormArgs& a, hipStream_t s);
+
+struct PromptArgs {
+    int32_t n_tokens, heads, kv_heads, n_seqs, max_tokens, window;
+    const void *q, *k, *v;
+    int64_t q_stride, q_head, k_stride, k_head, v_stride, v_head;
+    const int32_t* offsets;
+    float scale;
+    void* out;
+    int32_t* status;
+};
+// Whether the workgroups of a call can be counted in 31 bits.
+bool prompt_fits(const PromptArgs& a);
+hipError_t launch_prompt(int type, int head_dim, const PromptArgs& a, hipStream_t s);
+
+struct QuantizeArgs {
+    int32_t rows, k;
+    const void* x;
+    int64_t x_stride;
+    uint8_t* codes;
+    int64_t code_stride;
+    float* scales;
+};
+hipError_t launch_quantize(int type, int block_rows, const QuantizeArgs& a, hipStream_t s);
+
+struct F8Args {
+    int32_t rows, n, k, act;
+    const void* x;
+    int64_t x_stride;
+    const float* x_scales;
+    const uint8_t* codes;
+    int64_t code_stride;
+    const float* scales;
+    const void *bias;
+    void *y;
+    int64_t y_stride;
+    void* workspace;
+};
+// Workspace bytes of launch_f8; 0 where it needs none.
+size_t f8_workspace(int32_t rows, int32_t n, int32_t k, int32_t act);
+hipError_t launch_f8(int type, const F8Args& a, hipStream_t s);
 
 }  // namespace rm
