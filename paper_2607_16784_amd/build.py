@@ -27,6 +27,12 @@ def hipcc() -> str:
     return cand if os.path.exists(cand) else (shutil.which("hipcc") or "hipcc")
 
 
+# Matrix instructions write arch registers, where vector instructions can read
+# them; left to itself the compiler of a kernel with one wave a SIMD has them write
+# accumulation registers and moves every product.
+EXTRA = {"f8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+
+
 def compile_flags():
     return ["--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -44,7 +50,8 @@ def build(verbose: bool = False) -> str:
     procs = []
     for src in srcs:
         obj = os.path.join(objdir, os.path.basename(src)[:-4] + ".o")
-        cmd = [hipcc()] + compile_flags() + ["-c", src, "-o", obj]
+        cmd = [hipcc()] + compile_flags() + EXTRA.get(os.path.basename(src), [])
+        cmd += ["-c", src, "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE,

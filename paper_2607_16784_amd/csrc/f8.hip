@@ -12,9 +12,8 @@
 // round the waves of a workgroup, x is quantised in the registers of the wave that
 // multiplies it, and the waves' totals are joined through LDS.
 //
-// Many rows (tile_kernel): x is quantised once into the workspace and passes
-// through LDS, 64 weight rows a wave straight into registers, both a step of 128
-// columns or more ahead.
+// Many rows (tile_kernel): x is quantised once into the workspace, then tiles of
+// both go through LDS, a step of 128 columns or more ahead.
 #include "rm_common.h"
 #include "rm_decode.h"
 
@@ -102,8 +101,8 @@ __device__ inline float row16_max(float v)
     return MaxNan::of(v, dpp_float<0x140>(v));
 }
 
-// Blocks of one row: 16 lanes a block, 16 blocks a workgroup.  PACK: rows of whole
-// blocks (zeros behind k) and scales block by block, as tile_kernel reads them.
+// Blocks of one row: 16 lanes a block, 16 blocks a workgroup.  PACK: codes (zeros
+// behind k) and scales block by block, as tile_kernel reads them.
 template <typename T, bool PACK>
 __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs a, int32_t blocks)
 {
@@ -117,7 +116,8 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs a, int32_t b
             load_some(static_cast<const T*>(a.x) + row * a.x_stride + c, a.k - c);
         const int e = scale_exponent(row16_max(largest8<T>(0.0f, v)));
         const u32x2 code = codes8<T>(v, inverse_from(e));
-        uint8_t* out = a.codes + row * a.code_stride + c;
+        uint8_t* out = PACK ? a.codes + ((int64_t)block * a.rows + row) * kBlock + t * 8
+                            : a.codes + row * a.code_stride + c;
         typedef u32x2 V __attribute__((aligned(1)));
         if (PACK || c + 8 <= a.k) {
             *reinterpret_cast<V*>(out) = code;
@@ -188,8 +188,9 @@ __global__ __launch_bounds__(256) void pack_kernel(F8Args a, int32_t blocks, uin
         const int block = (int)(at - row * blocks), c = block * kBlock + t * 16;
         const u32x4 v = load16_some(static_cast<const uint8_t*>(a.x) + row * a.x_stride + c,
                                     a.k - c);
-        *reinterpret_cast<u32x4*>(codes + row * (int64_t)blocks * kBlock + c) = v;
-        if (t == 0) scales[(int64_t)block * a.rows + row] = a.x_scales[at];
+        const int64_t to = (int64_t)block * a.rows + row;
+        *reinterpret_cast<u32x4*>(codes + to * kBlock + t * 16) = v;
+        if (t == 0) scales[to] = a.x_scales[at];
     }
 }
 
@@ -340,15 +341,17 @@ __global__ __launch_bounds__(few_waves(NT, MT) * 64) void few_kernel(F8Args a, i
 
 // ---- many rows -------------------------------------------------------------
 
-constexpr int kWaves = 4;       // of a tile, side by side along the outputs
-
 // x as quantize_kernel packs it.
 struct Packed {
-    const uint8_t* codes;       // [rows][blocks * 128]
+    const uint8_t* codes;       // [blocks][rows][128]
     const float* scales;        // [blocks][rows]
     int32_t blocks;
-    int64_t tiles, tiles_m, first;
+    uint32_t tiles, tiles_m, first;      // 31 bits: y has a tile's outputs for each
 };
+
+// Bytes of a step in LDS: codes of the weights and of x, scales of x and 64 of the
+// weights (two a wave, and what the other lanes of their load bring).
+constexpr int tile_stage(int weights, int rows) { return (weights + rows) * kBlock + rows * 4 + 256; }
 
 // 16 bytes a lane from base + offset to LDS, lane by lane behind each other.  Not
 // the builtin: the compiler would wait for all of it before the next read of LDS.
@@ -358,130 +361,188 @@ __device__ inline void to_lds16(uint32_t lds, uint32_t offset, const uint8_t* ba
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                  :: "s"(lds), "v"(offset), "s"(base) : "memory");
 }
-__device__ inline void to_lds4(uint32_t lds, uint32_t offset, const void* base)
+// 4 bytes a lane from an address of its own.
+__device__ inline void to_lds4(uint32_t lds, const void* from)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
-                 :: "s"(lds), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+                 :: "s"(lds), "v"(from) : "memory");
+}
+// An address that all lanes agree on, in scalar registers.
+__device__ inline const uint8_t* scalar(const uint8_t* p)
+{
+    const uint64_t v = (uint64_t)(uintptr_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
+    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    return (const uint8_t*)(uintptr_t)((uint64_t)hi << 32 | lo);
 }
 __device__ inline uint32_t lds_address(const void* p)
 {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
 
-// TN x 16 weight rows a wave, TM x 16 rows of x a workgroup, SETS steps in flight.
-template <typename T, int TN, int TM, int SETS, bool GATED>
-__global__ __launch_bounds__(kWaves * 64) void tile_kernel(F8Args a, Packed x)
+// TN x 16 weight rows and TM x 16 rows of x a wave, WN x WM waves a workgroup.
+//
+// Both operands pass through LDS, STAGES steps of 128 columns in a ring.  A step has
+// one barrier, in front of its last 16 rows of x: what it has read is free then, the
+// next step is there, and that one's weights and first rows are read beside the last
+// matrix instructions.  A product goes into its total kLag matrix instructions
+// behind its own, so that no vector instruction waits for one.
+// ALIGNED: weights by 16 bytes at addresses that are multiples of it, whole blocks;
+// they go to LDS directly, others through registers.
+template <typename T, int WN, int WM, int TN, int TM, int STAGES, bool GATED, bool ALIGNED>
+__global__ __launch_bounds__(WN * WM * 64) __attribute__((amdgpu_waves_per_eu(2))) void
+tile_kernel(F8Args a, Packed x)
 {
-    constexpr int MB = TM * 16, STAGE = MB * kBlock, GROUPS = MB / 8 / kWaves;
-    extern __shared__ __align__(1024) uint8_t lds[];          // [SETS][STAGE], [SETS][MB] scales
-    float* lds_scales = reinterpret_cast<float*>(lds + SETS * STAGE);
+    constexpr int WAVES = WN * WM, NB = WN * TN * 16, MB = WM * TM * 16;
+    constexpr int W_GROUPS = NB / 8 / WAVES, X_GROUPS = MB / 8 / WAVES;    // of 8 rows
+    constexpr int X_AT = NB * kBlock, S_AT = X_AT + MB * kBlock;
+    constexpr int STAGE = tile_stage(NB, MB);
+    constexpr int LOADS = (ALIGNED ? W_GROUPS : 0) + X_GROUPS + 2;
+    static_assert(NB % (8 * WAVES) == 0 && MB % (8 * WAVES) == 0, "groups");
+    static_assert((STAGES - 2) * LOADS < 64, "s_waitcnt counts 63 loads");
+    extern __shared__ __align__(1024) uint8_t lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int li = lane & 15, quad = lane >> 4;
+    const int li = lane & 15, quad = lane >> 4, wn = wave % WN, wm = wave / WN;
 
     // The XCDs take the workgroups in turn; each gets tiles behind each other, four
     // of x beside each other, so that its L2 holds what they share.
-    const int64_t per = (x.tiles + 7) / 8, block_at = x.first + blockIdx.x;
-    const int64_t at = block_at % 8 * per + block_at / 8;
+    const uint32_t per = (x.tiles + 7) / 8, block_at = x.first + blockIdx.x;
+    const uint32_t at = block_at % 8 * per + block_at / 8;
     if (block_at / 8 >= per || at >= x.tiles) return;
-    const int64_t tiles_n = x.tiles / x.tiles_m, group = at / (4 * tiles_n);
-    const int64_t wide = min((int64_t)4, x.tiles_m - group * 4), in = at - group * 4 * tiles_n;
-    const int64_t m0 = (group * 4 + in % wide) * MB;
-    const Runs<GATED> runs(in / wide * kWaves + wave, TN * 16, a.n);
+    const uint32_t tiles_n = x.tiles / x.tiles_m, group = at / (4 * tiles_n);
+    const uint32_t wide = min(4u, x.tiles_m - group * 4), in = at - group * 4 * tiles_n;
+    const int tile_n = __builtin_amdgcn_readfirstlane((int)(in / wide));
+    const int m0 = __builtin_amdgcn_readfirstlane((int)((group * 4 + in % wide) * MB));
 
-    const uint8_t* w[TN];
+    // Sources of the loads.  A chunk of 16 columns lies at (chunk ^ row) % 8 of its
+    // row in LDS, so that the 16 rows of an operand are spread over the banks.
+    const int row8 = lane >> 3, chunk = ((lane & 7) ^ row8) * 16;
+    const uint8_t* w_base[W_GROUPS];
+    uint32_t w_from[W_GROUPS], x_from[X_GROUPS];
 #pragma unroll
-    for (int t = 0; t < TN; ++t) {
-        const int r = t * 16 + li, run = t >= TN / 2;
-        w[t] = a.codes + min(runs.row[run] + r % (TN * 8), runs.last[run]) * a.code_stride +
-               quad * 16;
+    for (int i = 0; i < W_GROUPS; ++i) {
+        const int r = (i * WAVES + wave) * 8;             // all 8 in one run
+        const Runs<GATED> runs((int64_t)tile_n * WN + r / (TN * 16), TN * 16, a.n);
+        const int run = r % (TN * 16) / (TN * 8);
+        const int64_t row = min(runs.row[run] + r % (TN * 8), runs.last[run]);
+        w_base[i] = scalar(a.codes + row * a.code_stride);
+        w_from[i] = (uint32_t)(min((int64_t)row8, runs.last[run] - row) * a.code_stride) + chunk;
     }
-    const float* scale0 = a.scales + (int64_t)runs.scale[0] * x.blocks;
-    const float* scale1 = a.scales + (int64_t)runs.scale[1] * x.blocks;
-    // a chunk of 16 columns lies at (chunk ^ row) % 8 of its row in LDS, so that the
-    // 16 rows of an operand are spread over the banks
-    const int64_t pitch = (int64_t)x.blocks * kBlock;
-    const uint8_t* x_base = x.codes + m0 * pitch;
-    const float* s_base = x.scales + m0;
-    uint32_t from[GROUPS];
+    const uint8_t* x_base = scalar(x.codes + (int64_t)m0 * kBlock);
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) {
-        const int r = (i * kWaves + wave) * 8 + (lane >> 3);
-        from[i] = (uint32_t)(min((int64_t)r, a.rows - 1 - m0) * pitch) +
-                  (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16);
+    for (int i = 0; i < X_GROUPS; ++i) {
+        const int r = (i * WAVES + wave) * 8 + row8;
+        x_from[i] = (uint32_t)(min(r, a.rows - 1 - m0) * kBlock + chunk);
     }
-    const int s_row = wave * 64 % MB + lane;
-    const uint32_t s_from = (uint32_t)min((int64_t)(s_row % MB), a.rows - 1 - m0) * 4;
-    const uint32_t x_lds = __builtin_amdgcn_readfirstlane(lds_address(lds));
-    const uint32_t s_lds = __builtin_amdgcn_readfirstlane(lds_address(lds_scales));
+    // scales: of x's rows, 64 a wave and round again, and two of each wave's weights
+    const int s_row = (wave * 64 + lane) % MB;
+    const float* xs_base = x.scales + m0 + min(s_row, a.rows - 1 - m0);
+    const Runs<GATED> mine((int64_t)tile_n * WN + lane / 2 % WN, TN * 16, a.n);
+    const float* ws_base = a.scales + (int64_t)mine.scale[lane & 1] * x.blocks;
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(lds));
 
-    u32x4 wq[SETS][TN][2];
-    float sw0[SETS], sw1[SETS];
-    auto fetch = [&](int step, int set) {
-        const uint8_t* base = x_base + (int64_t)step * kBlock;
+    u32x4 kept[ALIGNED ? 1 : W_GROUPS];
+    auto fetch = [&](int step, int stage) {
+        const uint32_t to = lds0 + stage * STAGE;
+        const int64_t c = (int64_t)step * kBlock, rows_at = (int64_t)step * a.rows;
 #pragma unroll
-        for (int i = 0; i < GROUPS; ++i)
-            to_lds16(x_lds + set * STAGE + (i * kWaves + wave) * 1024, from[i], base);
-        to_lds4(s_lds + set * (MB * 4) + wave * 64 % MB * 4, s_from,
-                s_base + (int64_t)step * a.rows);
-        const int c = step * kBlock;
-        if (c + kBlock <= a.k) {
+        for (int i = 0; i < X_GROUPS; ++i)
+            to_lds16(to + X_AT + (i * WAVES + wave) * 1024, x_from[i], x_base + rows_at * kBlock);
+        to_lds4(to + S_AT + wave * 64 % MB * 4, xs_base + rows_at);
+        to_lds4(to + S_AT + MB * 4, ws_base + step);
 #pragma unroll
-            for (int t = 0; t < TN; ++t)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) wq[set][t][h] = load16(w[t] + c + h * 64);
-        } else {
-#pragma unroll
-            for (int t = 0; t < TN; ++t)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    wq[set][t][h] = load16_some(w[t] + c + h * 64, a.k - c - quad * 16 - h * 64);
+        for (int i = 0; i < W_GROUPS; ++i) {
+            if (ALIGNED) to_lds16(to + (i * WAVES + wave) * 1024, w_from[i], w_base[i] + c);
+            else kept[ALIGNED ? 0 : i] = load16_some(w_base[i] + w_from[i] + c, a.k - c - chunk);
         }
-        sw0[set] = scale0[step];
-        sw1[set] = scale1[step];
     };
-    f32x4 acc[TN][TM] = {};
-    const int swizzle0 = (quad ^ (li & 7)) * 16, swizzle1 = ((quad + 4) ^ (li & 7)) * 16;
-    auto multiply = [&](int set) {
-        const uint8_t* stage = lds + set * STAGE + li * kBlock;
-        const float* scales = lds_scales + set * MB + li;
+    auto put = [&](int stage) {
+#pragma unroll
+        for (int i = 0; i < (ALIGNED ? 0 : W_GROUPS); ++i)
+            *reinterpret_cast<u32x4*>(lds + stage * STAGE + (i * WAVES + wave) * 1024 + lane * 16) =
+                kept[i];
+    };
+    const int swizzle0 = li * kBlock + (quad ^ (li & 7)) * 16;
+    const int swizzle1 = li * kBlock + ((quad + 4) ^ (li & 7)) * 16;
+    auto sixteen = [&](const uint8_t* from) {
+        return operand(*reinterpret_cast<const u32x4*>(from + swizzle0),
+                       *reinterpret_cast<const u32x4*>(from + swizzle1));
+    };
+    auto rows_of = [&](int stage, int m, i32x8& v, float& s) {
+        const uint8_t* from = lds + stage * STAGE;
+        v = sixteen(from + X_AT + (wm * TM + m) * 2048);
+        s = *reinterpret_cast<const float*>(from + S_AT + ((wm * TM + m) * 16 + li) * 4);
+    };
+    i32x8 wq[TN];
+    float sw0, sw1;
+    auto weights_of = [&](int stage, int t) {
+        wq[t] = sixteen(lds + stage * STAGE + (wn * TN + t) * 2048);
+    };
+    auto weight_scales_of = [&](int stage) {
+        const float* s = reinterpret_cast<const float*>(lds + stage * STAGE + S_AT + MB * 4);
+        sw0 = s[wn * 2];
+        sw1 = GATED ? s[wn * 2 + 1] : sw0;
+    };
+
+    constexpr int kLag = TN < 3 ? TN : 3, kRing = 4;
+    static_assert(TN * TM % kRing == 0 && kLag < kRing && TM % 2 == 0, "rings");
+    f32x4 acc[TN][TM] = {}, p[kRing] = {};
+    i32x8 xm[2];
+    float sx[2], s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) {
+        fetch(min(i, x.blocks - 1), i);
+        put(i);
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    fetch(min(STAGES - 1, x.blocks - 1), STAGES - 1);
+#pragma unroll
+    for (int t = 0; t < TN; ++t) weights_of(0, t);
+    weight_scales_of(0);
+    rows_of(0, 0, xm[0], sx[0]);
+    int stage = 0;
+    for (int step = 0; step < x.blocks; ++step) {
+        const int following = stage == STAGES - 1 ? 0 : stage + 1;
 #pragma unroll
         for (int m = 0; m < TM; ++m) {
-            const u32x4 lo = *reinterpret_cast<const u32x4*>(stage + m * 16 * kBlock + swizzle0);
-            const u32x4 hi = *reinterpret_cast<const u32x4*>(stage + m * 16 * kBlock + swizzle1);
-            const float sx = scales[m * 16], s0 = sx * sw0[set], s1 = sx * sw1[set];
-            const i32x8 xm = operand(lo, hi);
+            if (m == TM - 1) {
+                put(stage == 0 ? STAGES - 1 : stage - 1);
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier"
+                             :: "n"((STAGES - 2) * LOADS) : "memory");
+                // behind the last step the last one again: a branch would part the
+                // matrix instructions from what stands between them
+                fetch(min(step + STAGES, x.blocks - 1), stage);
+            }
+            rows_of(m + 1 < TM ? stage : following, (m + 1) % TM, xm[(m + 1) & 1], sx[(m + 1) & 1]);
+            const float before0 = s0, before1 = s1;
+            s0 = sx[m & 1] * sw0, s1 = GATED ? sx[m & 1] * sw1 : s0;
+            if (m == TM - 1) weight_scales_of(following);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < TN; ++t) {
-                const f32x4 p = products(operand(wq[set][t][0], wq[set][t][1]), xm);
+                const int j = m * TN + t, done = (j - kLag + TN * TM) % (TN * TM);
+                p[j % kRing] = products(wq[t], xm[m & 1]);
+                if (m == TM - 1) weights_of(following, t);
+                const float s = done / TN == m ? (done % TN < TN / 2 ? s0 : s1)
+                                               : (done % TN < TN / 2 ? before0 : before1);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    acc[t][m][i] = __builtin_fmaf(p[i], t < TN / 2 ? s0 : s1, acc[t][m][i]);
+                    acc[done % TN][done / TN][i] = __builtin_fmaf(p[done % kRing][i], s,
+                                                                  acc[done % TN][done / TN][i]);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-    };
-    // In flight before a step: SETS - 1 steps of GROUPS + 1 + 2 TN loads; the oldest
-    // has to be there, and what the step before has read may be overwritten behind
-    // the barrier.
-    constexpr int LOADS = GROUPS + 1 + 2 * TN, AHEAD = (SETS - 2) * LOADS;
-    static_assert(AHEAD < 64, "s_waitcnt counts 63 loads");
-#pragma unroll
-    for (int i = 0; i < SETS - 1; ++i)
-        if (i < x.blocks) fetch(i, i);
-    for (int step = 0; step < x.blocks; step += SETS) {
-#pragma unroll
-        for (int set = 0; set < SETS; ++set) {
-            if (step + set >= x.blocks) break;
-            // behind the last fetch fewer are in flight
-            if (AHEAD > 0 && step + set + SETS - 1 <= x.blocks)
-                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(AHEAD) : "memory");
-            else
-                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            if (step + set + SETS - 1 < x.blocks)
-                fetch(step + set + SETS - 1, (set + SETS - 1) % SETS);
-            multiply(set);
-        }
+        stage = following;
     }
+#pragma unroll
+    for (int j = TN * TM - kLag; j < TN * TM; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            acc[j % TN][j / TN][i] = __builtin_fmaf(p[j % kRing][i], j % TN < TN / 2 ? s0 : s1,
+                                                    acc[j % TN][j / TN][i]);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // LDS is this workgroup's until here
 
+    const Runs<GATED> runs((int64_t)tile_n * WN + wn, TN * 16, a.n);
     const T* bias = static_cast<const T*>(a.bias);
     const int64_t outs = GATED ? a.n / 2 : a.n;
     constexpr int OUT = GATED ? TN / 2 : TN;
@@ -497,7 +558,7 @@ __global__ __launch_bounds__(kWaves * 64) void tile_kernel(F8Args a, Packed x)
         }
 #pragma unroll
         for (int m = 0; m < TM; ++m) {
-            const int64_t row = m0 + m * 16 + li;
+            const int64_t row = (int64_t)m0 + (wm * TM + m) * 16 + li;
             if (row >= a.rows) continue;
             typedef T V4 __attribute__((ext_vector_type(4)));
             typedef V4 V4u __attribute__((aligned(2)));
@@ -522,6 +583,9 @@ __global__ __launch_bounds__(kWaves * 64) void tile_kernel(F8Args a, Packed x)
 // ---- launches --------------------------------------------------------------
 
 constexpr int kFewRows = 64;       // the most rows that few_kernel takes
+
+// tile_kernel counts the bytes of 8 rows of weights in 32 bits
+bool few(int32_t rows, int64_t code_stride) { return rows <= kFewRows || code_stride >= 1 << 28; }
 
 int blocks_of(int32_t k) { return (k + kBlock - 1) / kBlock; }
 
@@ -559,27 +623,45 @@ hipError_t launch_few(const F8Args& a, hipStream_t s)
     return launch_few_rows<T, 4, GIVEN, GATED>(a, s);
 }
 
-template <typename T, int TN, int TM, int SETS, bool GATED>
+template <typename T, int WN, int WM, int TN, int TM, int STAGES, bool GATED, bool ALIGNED>
 hipError_t launch_tiles(const F8Args& a, Packed x, hipStream_t s)
 {
-    constexpr int MB = TM * 16, NB = kWaves * TN * 16;
-    x.tiles_m = ((int64_t)a.rows + MB - 1) / MB;
-    x.tiles = x.tiles_m * (((int64_t)a.n + NB - 1) / NB);
-    const size_t lds = (size_t)SETS * MB * (kBlock + 4);
-    auto kernel = tile_kernel<T, TN, TM, SETS, GATED>;
+    constexpr int MB = WM * TM * 16, NB = WN * TN * 16, THREADS = WN * WM * 64;
+    const int64_t tiles_m = ((int64_t)a.rows + MB - 1) / MB;
+    const int64_t tiles = tiles_m * (((int64_t)a.n + NB - 1) / NB);
+    if (tiles > 0x7fffff00) return hipErrorInvalidConfiguration;
+    x.tiles_m = (uint32_t)tiles_m;
+    x.tiles = (uint32_t)tiles;
+    constexpr size_t lds = (size_t)STAGES * tile_stage(NB, MB);
+    auto kernel = tile_kernel<T, WN, WM, TN, TM, STAGES, GATED, ALIGNED>;
     if (lds > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize,
                                                  (int)lds);
         if (e != hipSuccess) return e;
     }
-    const int64_t all = (x.tiles + 7) / 8 * 8, most = most_blocks(kWaves * 64) / 8 * 8;
-    for (x.first = 0; x.first < all; x.first += most) {
-        const int64_t n = all - x.first < most ? all - x.first : most;
-        const hipError_t e = launch(kernel, dim3((unsigned)n), kWaves * 64, lds, s, a, x);
+    const int64_t all = (tiles + 7) / 8 * 8, most = most_blocks(THREADS) / 8 * 8;
+    for (int64_t first = 0; first < all; first += most) {
+        x.first = (uint32_t)first;
+        const int64_t n = all - first < most ? all - first : most;
+        const hipError_t e = launch(kernel, dim3((unsigned)n), THREADS, lds, s, a, x);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
+}
+
+template <typename T, bool GATED, bool ALIGNED>
+hipError_t launch_sizes(const F8Args& a, const Packed& x, hipStream_t s)
+{
+    auto tiles = [&](int n, int rows) {
+        return (((int64_t)a.rows + rows - 1) / rows) * (((int64_t)a.n + n - 1) / n);
+    };
+    // registers hold no copy of unaligned weights beside the totals of a large tile
+    if (ALIGNED && tiles(256, 256) >= kComputeUnits / 2)
+        return launch_tiles<T, 4, 2, 4, 8, 2, GATED, true>(a, x, s);
+    if (tiles(128, 128) >= kComputeUnits * 3 / 4)
+        return launch_tiles<T, 2, 2, 4, 4, 3, GATED, ALIGNED>(a, x, s);
+    return launch_tiles<T, 4, 1, 2, 4, 4, GATED, ALIGNED>(a, x, s);
 }
 
 template <typename T, bool GATED>
@@ -596,24 +678,23 @@ hipError_t launch_many(const F8Args& a, hipStream_t s)
         e = launch(pack_kernel, dim3((unsigned)(n < most ? n : most)), 256, 0, s, a, blocks, codes,
                    scales);
     } else {
-        const QuantizeArgs q = {a.rows, a.k, a.x, a.x_stride, codes, (int64_t)blocks * kBlock,
-                                scales};
+        const QuantizeArgs q = {a.rows, a.k, a.x, a.x_stride, codes, 0, scales};
         const int64_t n = (all + 15) / 16;
         e = launch(quantize_kernel<T, true>, dim3((unsigned)(n < most ? n : most)), 256, 0, s, q,
                    blocks);
     }
     if (e != hipSuccess) return e;
     const Packed x = {codes, scales, blocks, 0, 0, 0};
-    const int64_t middle = (((int64_t)a.rows + 127) / 128) * (((int64_t)a.n + 255) / 256);
-    if (middle >= kComputeUnits) return launch_tiles<T, 4, 8, 2, GATED>(a, x, s);
-    return launch_tiles<T, 2, 4, 4, GATED>(a, x, s);
+    const bool aligned = ((uintptr_t)a.codes | (uintptr_t)a.code_stride | (uintptr_t)a.k) % 16 == 0 &&
+                         a.k % kBlock == 0;
+    return aligned ? launch_sizes<T, GATED, true>(a, x, s) : launch_sizes<T, GATED, false>(a, x, s);
 }
 
 template <typename T>
 hipError_t launch_type(const F8Args& a, hipStream_t s)
 {
     const bool gated = a.act == RM_ACT_SWIGLU;
-    if (a.rows > kFewRows) return gated ? launch_many<T, true>(a, s) : launch_many<T, false>(a, s);
+    if (!few(a.rows, a.code_stride)) return gated ? launch_many<T, true>(a, s) : launch_many<T, false>(a, s);
     if (a.x_scales) return gated ? launch_few<T, true, true>(a, s) : launch_few<T, true, false>(a, s);
     return gated ? launch_few<T, false, true>(a, s) : launch_few<T, false, false>(a, s);
 }
@@ -634,7 +715,7 @@ hipError_t launch_quantize_type(int block_rows, const QuantizeArgs& a, hipStream
 size_t f8_workspace(int32_t rows, int32_t n, int32_t k, int32_t act)
 {
     (void)n, (void)act;
-    if (rows <= kFewRows) return 0;
+    if (few(rows, 0)) return 0;
     const size_t blocks = (size_t)blocks_of(k);
     return ((size_t)rows * blocks * kBlock + 255) / 256 * 256 + (size_t)rows * blocks * 4;
 }
