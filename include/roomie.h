@@ -131,7 +131,7 @@ extern "C" {
 #define RM_MAX_SEQUENCES     65535  /* n_seqs of the cache calls and prompts   */
 #define RM_MAX_HEAD_WIDTH      512  /* head_dim of rm_head_norm_rotary         */
 #define RM_MAX_F8_COLUMNS  2097152  /* k of rm_f8_linear and rm_f8_quantize    */
-#define RM_MAX_F8_OUTPUTS 536870848 /* n of rm_f8_linear                       */
+#define RM_MAX_F8_OUTPUTS  67108864 /* n of rm_f8_linear                       */
 #define RM_MAX_F8_ROWS     4194240  /* rows of rm_f8_linear                    */
 
 /* Target-device descriptor: the SM limits of Eq. (1) and Eq. (2).

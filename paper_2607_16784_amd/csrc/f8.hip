@@ -8,11 +8,11 @@
 // long as both operands keep it: lane l has the bytes 16 (l / 16) .. and
 // 64 + 16 (l / 16) .. of its row.
 //
-// Few rows of x (few_kernel): bound by reading the codes once.  The blocks go
+// Up to 16 rows of x (few_kernel): bound by reading the codes once.  The blocks go
 // round the waves of a workgroup, x is quantised in the registers of the wave that
 // multiplies it, and the waves' totals are joined through LDS.
 //
-// Many rows (tile_kernel): x is quantised once into the workspace, then tiles of
+// More (tile_kernel): x is quantised once into the workspace, then tiles of
 // both go through LDS, a step of 128 columns or more ahead.
 #include "rm_common.h"
 #include "rm_decode.h"
@@ -49,28 +49,75 @@ __device__ inline int scale_exponent(float top)
 }
 __device__ inline float power_of(int biased) { return __builtin_bit_cast(float, biased << 23); }
 __device__ inline float scale_from(int e) { return e ? power_of(e) : __builtin_nanf(""); }
-// 1 / scale; what is not finite stays so
-__device__ inline float inverse_from(int e) { return power_of(254 - (e ? e : 127)); }
+// the divisor of the codes; where the scale is NaN they do not count
+__device__ inline float divisor_from(int e) { return power_of(e ? e : 127); }
 
-__device__ inline uint32_t codes4(float a, float b, float c, float d)
+// Largest magnitudes as bits, which are in the numbers' order with infinities and
+// NaN above them.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ inline uint32_t larger(uint32_t a, uint32_t b)       // of two pairs
 {
-    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a),
+                                                                  __builtin_bit_cast(u16x2, b)));
 }
-
 template <typename T>
-__device__ inline u32x2 codes8(typename Vec<T>::x8 v, float inv)
+__device__ inline uint32_t largest8(uint32_t top, typename Vec<T>::x8 v)
 {
-    return u32x2{codes4((float)v[0] * inv, (float)v[1] * inv, (float)v[2] * inv, (float)v[3] * inv),
-                 codes4((float)v[4] * inv, (float)v[5] * inv, (float)v[6] * inv, (float)v[7] * inv)};
-}
-
-template <typename T>
-__device__ inline float largest8(float top, typename Vec<T>::x8 v)
-{
+    const u32x4 w = __builtin_bit_cast(u32x4, v);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = MaxNan::of(top, fabsf((float)v[i]));
+    for (int i = 0; i < 4; ++i) top = larger(top, w[i] & 0x7fff7fffu);
     return top;
+}
+template <typename T>
+__device__ inline float largest_of(uint32_t pair)
+{
+    const uint16_t top = (uint16_t)max(pair & 0xffffu, pair >> 16);
+    return (float)__builtin_bit_cast(T, top);
+}
+template <int CTRL>
+__device__ inline uint32_t dpp_bits(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xF, 0xF, false);
+}
+// Largest pairs of 16 neighbouring lanes.
+__device__ inline uint32_t row16_larger(uint32_t v)
+{
+    v = larger(v, dpp_bits<0xB1>(v));
+    v = larger(v, dpp_bits<0x4E>(v));
+    v = larger(v, dpp_bits<0x141>(v));
+    return larger(v, dpp_bits<0x140>(v));
+}
+// Of the four lanes 16 apart, for every lane.
+__device__ inline uint32_t rows_larger(uint32_t v)
+{
+    const auto h = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    const uint32_t h0 = h[0], h1 = h[1], w = larger(h0, h1);
+    const auto r = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    const uint32_t r0 = r[0], r1 = r[1];
+    return larger(r0, r1);
+}
+
+// Codes of eight values by the hardware's conversion, which divides by the power of
+// two `scale` and rounds once.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+__device__ inline uint32_t codes4(bf16x2 a, bf16x2 b, float scale)
+{
+    const s16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(s16x2{0, 0}, a, scale, false);
+    return __builtin_bit_cast(uint32_t,
+                              __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, b, scale, true));
+}
+__device__ inline uint32_t codes4(f16x2 a, f16x2 b, float scale)
+{
+    const s16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(s16x2{0, 0}, a, scale, false);
+    return __builtin_bit_cast(uint32_t,
+                              __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(lo, b, scale, true));
+}
+template <typename T>
+__device__ inline u32x2 codes8(typename Vec<T>::x8 v, float scale)
+{
+    typedef typename Vec<T>::x2 V2;
+    return u32x2{codes4(V2{v[0], v[1]}, V2{v[2], v[3]}, scale),
+                 codes4(V2{v[4], v[5]}, V2{v[6], v[7]}, scale)};
 }
 
 // 16 bytes of codes at any alignment.
@@ -79,27 +126,28 @@ __device__ inline u32x4 load16(const uint8_t* p)
     typedef u32x4 V __attribute__((aligned(1)));
     return *reinterpret_cast<const V*>(p);
 }
-// The first n (may be <= 0) of 16 codes, zeros behind them.
-__device__ inline u32x4 load16_some(const uint8_t* p, int64_t n)
+// The 16 bytes from byte c on of a row of `size` bytes, zeros behind its end: what the
+// end cuts off is the row's last 16 bytes moved down.
+__device__ inline u32x4 load16_of(const uint8_t* row, int64_t c, int64_t size)
 {
-    if (n >= 16) return load16(p);
-    u32x4 v = {};
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-        if (i < n) v[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
-    return v;
+    if (c + 16 <= size) return load16(row + c);
+    if (c >= size) return u32x4{0, 0, 0, 0};
+    uint64_t lo = 0, hi = 0;
+    if (size >= 16) {
+        const u32x4 v = load16(row + size - 16);
+        const int bits = (int)(c + 16 - size) * 8;        // 8 .. 120
+        lo = (uint64_t)v[1] << 32 | v[0];
+        hi = (uint64_t)v[3] << 32 | v[2];
+        lo = bits < 64 ? lo >> bits | hi << (64 - bits) : hi >> (bits - 64);
+        hi = bits < 64 ? hi >> bits : 0;
+    } else {
+        for (int i = 0; c + i < size; ++i)
+            (i < 8 ? lo : hi) |= (uint64_t)row[c + i] << (8 * (i & 7));
+    }
+    return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
 }
 
 // ---- codes and scales ------------------------------------------------------
-
-// Largest of 16 neighbouring lanes.
-__device__ inline float row16_max(float v)
-{
-    v = MaxNan::of(v, dpp_float<0xB1>(v));
-    v = MaxNan::of(v, dpp_float<0x4E>(v));
-    v = MaxNan::of(v, dpp_float<0x141>(v));
-    return MaxNan::of(v, dpp_float<0x140>(v));
-}
 
 // Blocks of one row: 16 lanes a block, 16 blocks a workgroup.  PACK: codes (zeros
 // behind k) and scales block by block, as tile_kernel reads them.
@@ -112,10 +160,12 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs a, int32_t b
         const bool small = all <= 0x7fffffff;       // wave-uniform
         const int64_t row = small ? (uint32_t)at / (uint32_t)blocks : at / blocks;
         const int block = (int)(at - row * blocks), c = block * kBlock + t * 8;
-        const typename Vec<T>::x8 v =
-            load_some(static_cast<const T*>(a.x) + row * a.x_stride + c, a.k - c);
-        const int e = scale_exponent(row16_max(largest8<T>(0.0f, v)));
-        const u32x2 code = codes8<T>(v, inverse_from(e));
+        const typename Vec<T>::x8 v = __builtin_bit_cast(
+            typename Vec<T>::x8,
+            load16_of(static_cast<const uint8_t*>(a.x) + 2 * row * a.x_stride, 2 * (int64_t)c,
+                      2 * (int64_t)a.k));
+        const int e = scale_exponent(largest_of<T>(row16_larger(largest8<T>(0, v))));
+        const u32x2 code = codes8<T>(v, divisor_from(e));
         uint8_t* out = PACK ? a.codes + ((int64_t)block * a.rows + row) * kBlock + t * 8
                             : a.codes + row * a.code_stride + c;
         typedef u32x2 V __attribute__((aligned(1)));
@@ -134,7 +184,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs a, int32_t b
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_square_kernel(QuantizeArgs a, int32_t blocks)
 {
-    __shared__ float part[2][4];
+    __shared__ uint32_t part[2][4];
     const int t = threadIdx.x & 15, r0 = threadIdx.x >> 4;
     const int64_t all = ((int64_t)a.rows + kBlock - 1) / kBlock * blocks;
     int turn = 0;
@@ -142,7 +192,7 @@ __global__ __launch_bounds__(256) void quantize_square_kernel(QuantizeArgs a, in
         const int64_t row = at / blocks * kBlock + r0;
         const int c = (int)(at % blocks) * kBlock + t * 8;
         typename Vec<T>::x8 v[8];
-        float top = 0.0f;
+        uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int64_t r = row + i * 16;
@@ -151,18 +201,17 @@ __global__ __launch_bounds__(256) void quantize_square_kernel(QuantizeArgs a, in
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) top = largest8<T>(top, v[i]);
-        top = wave_reduce<MaxNan>(top);
+        top = rows_larger(row16_larger(top));
         if ((threadIdx.x & 63) == 0) part[turn][threadIdx.x >> 6] = top;
         __syncthreads();
-        top = MaxNan::of(MaxNan::of(part[turn][0], part[turn][1]),
-                         MaxNan::of(part[turn][2], part[turn][3]));
-        const int e = scale_exponent(top);
-        const float inv = inverse_from(e);
+        top = larger(larger(part[turn][0], part[turn][1]), larger(part[turn][2], part[turn][3]));
+        const int e = scale_exponent(largest_of<T>(top));
+        const float divisor = divisor_from(e);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int64_t r = row + i * 16;
             if (r >= a.rows) continue;
-            const u32x2 code = codes8<T>(v[i], inv);
+            const u32x2 code = codes8<T>(v[i], divisor);
             uint8_t* out = a.codes + r * a.code_stride + c;
             typedef u32x2 V __attribute__((aligned(1)));
             if (c + 8 <= a.k) {
@@ -186,8 +235,7 @@ __global__ __launch_bounds__(256) void pack_kernel(F8Args a, int32_t blocks, uin
     for (int64_t at = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3); at < all; at += by) {
         const int64_t row = at / blocks;
         const int block = (int)(at - row * blocks), c = block * kBlock + t * 16;
-        const u32x4 v = load16_some(static_cast<const uint8_t*>(a.x) + row * a.x_stride + c,
-                                    a.k - c);
+        const u32x4 v = load16_of(static_cast<const uint8_t*>(a.x) + row * a.x_stride, c, a.k);
         const int64_t to = (int64_t)block * a.rows + row;
         *reinterpret_cast<u32x4*>(codes + to * kBlock + t * 16) = v;
         if (t == 0) scales[to] = a.x_scales[at];
@@ -225,109 +273,124 @@ __device__ inline float silu(float g) { return g / (1.0f + __expf(-g)); }
 
 // ---- few rows --------------------------------------------------------------
 
-// The most waves of a workgroup: totals of a wave are NT x MT x 1 KB of LDS.
-constexpr int few_waves(int nt, int mt) { return nt * mt >= 8 ? 4 : nt * mt >= 4 ? 8 : 16; }
+constexpr int kMostWaves = 8;
 
-// NT x 16 rows of the weights and MT x 16 of x a workgroup.
-template <typename T, int NT, int MT, bool GIVEN, bool GATED>
-__global__ __launch_bounds__(few_waves(NT, MT) * 64) void few_kernel(F8Args a, int32_t blocks)
+// NT x 16 rows of the weights, 16 of x a workgroup.  AHEAD: blocks of weights and of x
+// that a wave has in flight.
+template <typename T, int NT, int AHEAD, bool GIVEN, bool GATED>
+__global__ __launch_bounds__(kMostWaves * 64) void few_kernel(F8Args a, int32_t blocks)
 {
     typedef typename Vec<T>::x8 V;
-    extern __shared__ __align__(16) float part[];      // [waves][MT * 16][NT * 16 + 4]
     constexpr int PITCH = NT * 16 + 4;
+    __shared__ __align__(16) float part[kMostWaves][16 * PITCH];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6, li = lane & 15, quad = lane >> 4;
-    const int64_t tile = blockIdx.x;
-    const int m0 = blockIdx.y * (MT * 16);
-    const Runs<GATED> runs(tile, NT * 16, a.n);
+    const Runs<GATED> runs(blockIdx.x, NT * 16, a.n);
 
     const uint8_t* w[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const int r = t * 16 + li, run = r / (NT * 8);
-        w[t] = a.codes + min(runs.row[run] + r % (NT * 8), runs.last[run]) * a.code_stride;
+        const int r = t * 16 + li;
+        const bool second = r >= NT * 8;          // no index: runs stays in registers
+        w[t] = a.codes +
+               min((second ? runs.row[1] : runs.row[0]) + r % (NT * 8),
+                   second ? runs.last[1] : runs.last[0]) * a.code_stride;
     }
-    int64_t row[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) row[t] = min(m0 + t * 16 + li, a.rows - 1);
-    f32x4 acc[NT][MT] = {};
+    const int64_t row = min(li, a.rows - 1);
+    const uint8_t* x = static_cast<const uint8_t*>(a.x) +
+                       row * a.x_stride * (GIVEN ? 1 : 2);
+    const float* scale0 = a.scales + (int64_t)runs.scale[0] * blocks;
+    const float* scale1 = a.scales + (int64_t)runs.scale[1] * blocks;
+    f32x4 acc[NT] = {};
 
-    auto load_w = [&](int block, u32x4 (&v)[NT][2]) {
-        const int c = block * kBlock + quad * 16;
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int at = c + h * 64;
-                v[t][h] = (block + 1) * kBlock <= a.k ? load16(w[t] + at)
-                                                      : load16_some(w[t] + at, a.k - at);
-            }
+    // a block's weights, x and scales
+    constexpr int X = GIVEN ? 2 : 4;
+    auto column = [](int64_t c, int h) {          // byte of the h-th load of x
+        return GIVEN ? c + h * 64 : 2 * c + h / 2 * 128 + h % 2 * 16;
     };
-    u32x4 now[NT][2], next[NT][2];
-    if (wave < blocks) load_w(wave, now);
-    for (int block = wave; block < blocks; block += waves) {
-        if (block + waves < blocks) load_w(block + waves, next);
-        const float s0 = a.scales[(int64_t)runs.scale[0] * blocks + block];
-        const float s1 = a.scales[(int64_t)runs.scale[1] * blocks + block];
-        const int c = block * kBlock + quad * 16;
+    struct Block {
+        u32x4 w[NT][2], x[X];
+        float sx, s0, s1;
+    };
+    const int whole = a.k / kBlock;
+    auto load = [&](int block, Block& b) {
+        const int64_t c = block * kBlock + quad * 16;
+        if (block < whole) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            i32x8 x;
-            float sx;
-            if (GIVEN) {
-                const uint8_t* p = static_cast<const uint8_t*>(a.x) + row[m] * a.x_stride + c;
-                sx = a.x_scales[row[m] * blocks + block];
-                x = operand(load16_some(p, a.k - c), load16_some(p + 64, a.k - c - 64));
-            } else {
-                const T* p = static_cast<const T*>(a.x) + row[m] * a.x_stride + c;
-                V v[4];
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    const int off = (h >> 1) * 64 + (h & 1) * 8;
-                    v[h] = load_some(p + off, a.k - c - off);
-                }
-                float top = 0.0f;
+                for (int h = 0; h < 2; ++h) b.w[t][h] = load16(w[t] + c + h * 64);
 #pragma unroll
-                for (int h = 0; h < 4; ++h) top = largest8<T>(top, v[h]);
-                const int e = scale_exponent(rows_reduce<MaxNan>(top));
-                const float inv = inverse_from(e);
-                sx = scale_from(e);
-                u32x2 q[4];
+            for (int h = 0; h < X; ++h) b.x[h] = load16(x + column(c, h));
+        } else {
 #pragma unroll
-                for (int h = 0; h < 4; ++h) q[h] = codes8<T>(v[h], inv);
-                x = operand(u32x4{q[0][0], q[0][1], q[1][0], q[1][1]},
-                            u32x4{q[2][0], q[2][1], q[3][0], q[3][1]});
-            }
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const f32x4 p = products(operand(now[t][0], now[t][1]), x);
-                // NT 1: a lane's four outputs are of one run, lanes differ
-                const bool second = NT == 1 ? quad >= 2 : t >= NT / 2;
-                const float s = sx * (second ? s1 : s0);
+                for (int h = 0; h < 2; ++h) b.w[t][h] = load16_of(w[t], c + h * 64, a.k);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[t][m][i] = __builtin_fmaf(p[i], s, acc[t][m][i]);
-            }
+            for (int h = 0; h < X; ++h)
+                b.x[h] = load16_of(x, column(c, h), (int64_t)a.k * (GIVEN ? 1 : 2));
+        }
+        b.sx = GIVEN ? a.x_scales[row * blocks + block] : 0.0f;
+        b.s0 = scale0[block];
+        b.s1 = GATED || NT > 1 ? scale1[block] : b.s0;
+    };
+    auto multiply = [&](const Block& b) {
+        i32x8 xq;
+        float sx = b.sx;
+        if (GIVEN) {
+            xq = operand(b.x[0], b.x[1]);
+        } else {
+            uint32_t top = 0;
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+                top = largest8<T>(top, __builtin_bit_cast(V, b.x[h % X]));
+            const int e = scale_exponent(largest_of<T>(rows_larger(top)));
+            sx = scale_from(e);
+            u32x2 q[4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+                q[h] = codes8<T>(__builtin_bit_cast(V, b.x[h % X]), divisor_from(e));
+            xq = operand(u32x4{q[0][0], q[0][1], q[1][0], q[1][1]},
+                         u32x4{q[2][0], q[2][1], q[3][0], q[3][1]});
         }
 #pragma unroll
-        for (int t = 0; t < NT; ++t) now[t][0] = next[t][0], now[t][1] = next[t][1];
+        for (int t = 0; t < NT; ++t) {
+            const f32x4 p = products(operand(b.w[t][0], b.w[t][1]), xq);
+            // NT 1: a lane's four outputs are of one run, lanes differ
+            const bool second = NT == 1 ? quad >= 2 : t >= NT / 2;
+            const float s = sx * (second ? b.s1 : b.s0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[t][i] = __builtin_fmaf(p[i], s, acc[t][i]);
+        }
+    };
+    Block b[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (wave + i * waves < blocks) load(wave + i * waves, b[i]);
+    for (int block = wave; block < blocks; block += AHEAD * waves) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (block + i * waves >= blocks) break;
+            multiply(b[i]);
+            const int next = block + (i + AHEAD) * waves;
+            if (next < blocks) load(next, b[i]);
+        }
     }
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-            *reinterpret_cast<f32x4*>(part + ((size_t)wave * MT * 16 + m * 16 + li) * PITCH +
-                                      t * 16 + quad * 4) = acc[t][m];
+    for (int t = 0; t < NT; ++t)
+        *reinterpret_cast<f32x4*>(&part[wave][li * PITCH + t * 16 + quad * 4]) = acc[t];
     __syncthreads();
     constexpr int OUT = GATED ? NT * 8 : NT * 16;
     const int64_t outs = GATED ? a.n / 2 : a.n;
     const T* bias = static_cast<const T*>(a.bias);
-    for (int i = threadIdx.x; i < MT * 16 * OUT; i += blockDim.x) {
+    for (int i = threadIdx.x; i < a.rows * OUT; i += blockDim.x) {
         const int j = i % OUT, m = i / OUT;
         const int64_t to = runs.row[0] + j;
-        if (m0 + m >= a.rows || to >= outs) continue;
+        if (to >= outs) continue;
         float g = 0.0f, u = 0.0f;
         for (int v = 0; v < waves; ++v) {
-            const float* p = part + ((size_t)v * MT * 16 + m) * PITCH + j;
+            const float* p = &part[v][m * PITCH + j];
             g += p[0];
             if (GATED) u += p[NT * 8];
         }
@@ -335,7 +398,7 @@ __global__ __launch_bounds__(few_waves(NT, MT) * 64) void few_kernel(F8Args a, i
             g += (float)bias[to];
             if (GATED) u += (float)bias[outs + to];
         }
-        static_cast<T*>(a.y)[(int64_t)(m0 + m) * a.y_stride + to] = (T)(GATED ? silu(g) * u : g);
+        static_cast<T*>(a.y)[m * a.y_stride + to] = (T)(GATED ? silu(g) * u : g);
     }
 }
 
@@ -347,6 +410,10 @@ struct Packed {
     const float* scales;        // [blocks][rows]
     int32_t blocks;
     uint32_t tiles, tiles_m, first;      // 31 bits: y has a tile's outputs for each
+    // The columns of a tile are split over `parts` workgroups, whose totals join_kernel
+    // adds.
+    uint32_t parts;
+    f32x4* join;                // [parts][tiles][TN * TM][threads]
 };
 
 // Bytes of a step in LDS: codes of the weights and of x, scales of x and 64 of the
@@ -380,6 +447,59 @@ __device__ inline uint32_t lds_address(const void* p)
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
 
+// Bias, activation and the result of a wave's totals: outputs of tile `tile` of TN x 16
+// weight rows, rows of x from row0.
+template <typename T, int TN, int TM, bool GATED>
+__device__ inline void finish(const F8Args& a, int64_t tile, int row0, const f32x4 (&acc)[TN][TM])
+{
+    const int lane = threadIdx.x & 63, li = lane & 15, quad = lane >> 4;
+    const Runs<GATED> runs(tile, TN * 16, a.n);
+    const T* bias = static_cast<const T*>(a.bias);
+    const int64_t outs = GATED ? a.n / 2 : a.n;
+    constexpr int OUT = GATED ? TN / 2 : TN;
+#pragma unroll
+    for (int t = 0; t < OUT; ++t) {
+        const int64_t to = runs.row[0] + t * 16 + quad * 4;
+        float b0[4], b1[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool there = bias && to + i < outs;
+            b0[i] = there ? (float)bias[to + i] : 0.0f;
+            b1[i] = there && GATED ? (float)bias[outs + to + i] : 0.0f;
+        }
+#pragma unroll
+        for (int m = 0; m < TM; ++m) {
+            const int64_t row = (int64_t)row0 + m * 16 + li;
+            if (row >= a.rows) continue;
+            typedef T V4 __attribute__((ext_vector_type(4)));
+            typedef V4 V4u __attribute__((aligned(2)));
+            V4 o;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float g = acc[t][m][i] + b0[i];
+                o[i] = (T)(GATED ? silu(g) * (acc[(t + TN / 2) % TN][m][i] + b1[i]) : g);
+            }
+            T* y = static_cast<T*>(a.y) + row * a.y_stride + to;
+            if (to + 4 <= outs) {
+                *reinterpret_cast<V4u*>(y) = o;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (to + i < outs) y[i] = o[i];
+            }
+        }
+    }
+}
+
+// Output tile and row tile of a tile's number: four of x beside each other, so that an
+// L2 that is given tiles behind each other holds what they share.
+__device__ inline uint2 place_of(uint32_t tile, uint32_t tiles_n, uint32_t tiles_m)
+{
+    const uint32_t group = tile / (4 * tiles_n), in = tile - group * 4 * tiles_n;
+    const uint32_t wide = min(4u, tiles_m - group * 4);
+    return make_uint2(in / wide, group * 4 + in % wide);
+}
+
 // TN x 16 weight rows and TM x 16 rows of x a wave, WN x WM waves a workgroup.
 //
 // Both operands pass through LDS, STAGES steps of 128 columns in a ring.  A step has
@@ -404,19 +524,22 @@ tile_kernel(F8Args a, Packed x)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int li = lane & 15, quad = lane >> 4, wn = wave % WN, wm = wave / WN;
 
-    // The XCDs take the workgroups in turn; each gets tiles behind each other, four
-    // of x beside each other, so that its L2 holds what they share.
-    const uint32_t per = (x.tiles + 7) / 8, block_at = x.first + blockIdx.x;
-    const uint32_t at = block_at % 8 * per + block_at / 8;
-    if (block_at / 8 >= per || at >= x.tiles) return;
-    const uint32_t tiles_n = x.tiles / x.tiles_m, group = at / (4 * tiles_n);
-    const uint32_t wide = min(4u, x.tiles_m - group * 4), in = at - group * 4 * tiles_n;
-    const int tile_n = __builtin_amdgcn_readfirstlane((int)(in / wide));
-    const int m0 = __builtin_amdgcn_readfirstlane((int)((group * 4 + in % wide) * MB));
+    // The XCDs take the workgroups in turn; each gets tiles behind each other.
+    const uint32_t all = x.tiles * x.parts, per = (all + 7) / 8, block_at = x.first + blockIdx.x;
+    const uint32_t number = block_at % 8 * per + block_at / 8;
+    if (block_at / 8 >= per || number >= all) return;
+    const uint32_t part = number / x.tiles;
+    const uint2 place = place_of(number - part * x.tiles, x.tiles / x.tiles_m, x.tiles_m);
+    const int tile_n = __builtin_amdgcn_readfirstlane((int)place.x);
+    const int m0 = __builtin_amdgcn_readfirstlane((int)(place.y * MB));
+    // its blocks of columns
+    const int chunk = (x.blocks + x.parts - 1) / x.parts;
+    const int from_step = __builtin_amdgcn_readfirstlane((int)(part * chunk));
+    const int end = min(x.blocks, from_step + chunk);
 
     // Sources of the loads.  A chunk of 16 columns lies at (chunk ^ row) % 8 of its
     // row in LDS, so that the 16 rows of an operand are spread over the banks.
-    const int row8 = lane >> 3, chunk = ((lane & 7) ^ row8) * 16;
+    const int row8 = lane >> 3, column = ((lane & 7) ^ row8) * 16;
     const uint8_t* w_base[W_GROUPS];
     uint32_t w_from[W_GROUPS], x_from[X_GROUPS];
 #pragma unroll
@@ -426,13 +549,13 @@ tile_kernel(F8Args a, Packed x)
         const int run = r % (TN * 16) / (TN * 8);
         const int64_t row = min(runs.row[run] + r % (TN * 8), runs.last[run]);
         w_base[i] = scalar(a.codes + row * a.code_stride);
-        w_from[i] = (uint32_t)(min((int64_t)row8, runs.last[run] - row) * a.code_stride) + chunk;
+        w_from[i] = (uint32_t)(min((int64_t)row8, runs.last[run] - row) * a.code_stride);
     }
     const uint8_t* x_base = scalar(x.codes + (int64_t)m0 * kBlock);
 #pragma unroll
     for (int i = 0; i < X_GROUPS; ++i) {
         const int r = (i * WAVES + wave) * 8 + row8;
-        x_from[i] = (uint32_t)(min(r, a.rows - 1 - m0) * kBlock + chunk);
+        x_from[i] = (uint32_t)(min(r, a.rows - 1 - m0) * kBlock + column);
     }
     // scales: of x's rows, 64 a wave and round again, and two of each wave's weights
     const int s_row = (wave * 64 + lane) % MB;
@@ -452,8 +575,8 @@ tile_kernel(F8Args a, Packed x)
         to_lds4(to + S_AT + MB * 4, ws_base + step);
 #pragma unroll
         for (int i = 0; i < W_GROUPS; ++i) {
-            if (ALIGNED) to_lds16(to + (i * WAVES + wave) * 1024, w_from[i], w_base[i] + c);
-            else kept[ALIGNED ? 0 : i] = load16_some(w_base[i] + w_from[i] + c, a.k - c - chunk);
+            if (ALIGNED) to_lds16(to + (i * WAVES + wave) * 1024, w_from[i] + column, w_base[i] + c);
+            else kept[ALIGNED ? 0 : i] = load16_of(w_base[i] + w_from[i], c + column, a.k);
         }
     };
     auto put = [&](int stage) {
@@ -491,17 +614,17 @@ tile_kernel(F8Args a, Packed x)
     float sx[2], s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) {
-        fetch(min(i, x.blocks - 1), i);
+        fetch(min(from_step + i, end - 1), i);
         put(i);
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    fetch(min(STAGES - 1, x.blocks - 1), STAGES - 1);
+    fetch(min(from_step + STAGES - 1, end - 1), STAGES - 1);
 #pragma unroll
     for (int t = 0; t < TN; ++t) weights_of(0, t);
     weight_scales_of(0);
     rows_of(0, 0, xm[0], sx[0]);
     int stage = 0;
-    for (int step = 0; step < x.blocks; ++step) {
+    for (int step = from_step; step < end; ++step) {
         const int following = stage == STAGES - 1 ? 0 : stage + 1;
 #pragma unroll
         for (int m = 0; m < TM; ++m) {
@@ -511,7 +634,7 @@ tile_kernel(F8Args a, Packed x)
                              :: "n"((STAGES - 2) * LOADS) : "memory");
                 // behind the last step the last one again: a branch would part the
                 // matrix instructions from what stands between them
-                fetch(min(step + STAGES, x.blocks - 1), stage);
+                fetch(min(step + STAGES, end - 1), stage);
             }
             rows_of(m + 1 < TM ? stage : following, (m + 1) % TM, xm[(m + 1) & 1], sx[(m + 1) & 1]);
             const float before0 = s0, before1 = s1;
@@ -542,96 +665,106 @@ tile_kernel(F8Args a, Packed x)
                                                     acc[j % TN][j / TN][i]);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // LDS is this workgroup's until here
 
-    const Runs<GATED> runs((int64_t)tile_n * WN + wn, TN * 16, a.n);
-    const T* bias = static_cast<const T*>(a.bias);
-    const int64_t outs = GATED ? a.n / 2 : a.n;
-    constexpr int OUT = GATED ? TN / 2 : TN;
+    if (x.parts > 1) {
+        f32x4* to = x.join + ((int64_t)number * TN * TM * (WAVES * 64) + threadIdx.x);
 #pragma unroll
-    for (int t = 0; t < OUT; ++t) {
-        const int64_t to = runs.row[0] + t * 16 + quad * 4;
-        float b0[4], b1[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bool there = bias && to + i < outs;
-            b0[i] = there ? (float)bias[to + i] : 0.0f;
-            b1[i] = there && GATED ? (float)bias[outs + to + i] : 0.0f;
-        }
-#pragma unroll
-        for (int m = 0; m < TM; ++m) {
-            const int64_t row = (int64_t)m0 + (wm * TM + m) * 16 + li;
-            if (row >= a.rows) continue;
-            typedef T V4 __attribute__((ext_vector_type(4)));
-            typedef V4 V4u __attribute__((aligned(2)));
-            V4 o;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float g = acc[t][m][i] + b0[i];
-                o[i] = (T)(GATED ? silu(g) * (acc[(t + TN / 2) % TN][m][i] + b1[i]) : g);
-            }
-            T* y = static_cast<T*>(a.y) + row * a.y_stride + to;
-            if (to + 4 <= outs) {
-                *reinterpret_cast<V4u*>(y) = o;
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (to + i < outs) y[i] = o[i];
-            }
-        }
+        for (int j = 0; j < TN * TM; ++j) to[j * (WAVES * 64)] = acc[j % TN][j / TN];
+        return;
     }
+    finish<T, TN, TM, GATED>(a, (int64_t)tile_n * WN + wn, m0 + wm * TM * 16, acc);
+}
+
+// The totals of the parts of a tile, in the parts' order.
+template <typename T, int WN, int WM, int TN, int TM, bool GATED>
+__global__ __launch_bounds__(WN * WM * 64) void join_kernel(F8Args a, Packed x)
+{
+    constexpr int THREADS = WN * WM * 64;
+    const uint32_t tile = blockIdx.x, tiles_n = x.tiles / x.tiles_m;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m = blockIdx.y;            // of the wave's 16 rows of x
+    f32x4 acc[TN][1];
+#pragma unroll
+    for (int t = 0; t < TN; ++t) acc[t][0] = f32x4{0, 0, 0, 0};
+    // four parts in flight; behind the last one the last again, for nothing
+    for (uint32_t part = 0; part < x.parts; part += 4) {
+        f32x4 v[4][TN];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            const int64_t at = (int64_t)min(part + i, x.parts - 1) * x.tiles + tile;
+#pragma unroll
+            for (int t = 0; t < TN; ++t)
+                v[i][t] = x.join[(at * TN * TM + m * TN + t) * THREADS + threadIdx.x];
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+            for (int t = 0; t < TN; ++t)
+                if (part + i < x.parts) acc[t][0] += v[i][t];
+    }
+    const uint2 place = place_of(tile, tiles_n, x.tiles_m);
+    finish<T, TN, 1, GATED>(a, (int64_t)place.x * WN + wave % WN,
+                            (int)place.y * (WM * TM * 16) + (wave / WN * TM + m) * 16, acc);
 }
 
 // ---- launches --------------------------------------------------------------
 
-constexpr int kFewRows = 64;       // the most rows that few_kernel takes
+constexpr int kFewRows = 16;       // the most rows that few_kernel takes
 
 // tile_kernel counts the bytes of 8 rows of weights in 32 bits
 bool few(int32_t rows, int64_t code_stride) { return rows <= kFewRows || code_stride >= 1 << 28; }
 
 int blocks_of(int32_t k) { return (k + kBlock - 1) / kBlock; }
 
-template <typename T, int NT, int MT, bool GIVEN, bool GATED>
-hipError_t launch_few_form(const F8Args& a, hipStream_t s)
+size_t packed_bytes(int32_t rows, int32_t k)
 {
-    const int blocks = blocks_of(a.k), most = few_waves(NT, MT), waves = blocks < most ? blocks : most;
-    const int64_t tiles = (a.n + NT * 16 - 1) / (NT * 16);
-    const size_t lds = (size_t)waves * MT * 16 * (NT * 16 + 4) * 4;
-    auto kernel = few_kernel<T, NT, MT, GIVEN, GATED>;
-    if (lds > 65536) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                 (int)lds);
-        if (e != hipSuccess) return e;
-    }
-    const int32_t rows = (a.rows + MT * 16 - 1) / (MT * 16);
-    return launch(kernel, dim3((unsigned)tiles, (unsigned)rows), (unsigned)(waves * 64), lds, s, a,
-                  blocks);
+    return ((size_t)rows * blocks_of(k) * (kBlock + 4) + 255) / 256 * 256;
 }
 
-template <typename T, int MT, bool GIVEN, bool GATED>
-hipError_t launch_few_rows(const F8Args& a, hipStream_t s)
+int64_t tiles_of(int32_t rows, int32_t n, int weights, int height)
 {
-    if (a.n >= 64 * 2 * kComputeUnits) return launch_few_form<T, 4, MT, GIVEN, GATED>(a, s);
-    if (a.n >= 32 * 2 * kComputeUnits) return launch_few_form<T, 2, MT, GIVEN, GATED>(a, s);
-    return launch_few_form<T, 1, MT, GIVEN, GATED>(a, s);
+    return (((int64_t)rows + height - 1) / height) * (((int64_t)n + weights - 1) / weights);
+}
+
+// Tiles of 128 x 128 where they fill three quarters of the card; else of 128 x 64, their
+// columns in parts of 6 blocks or more where these do not fill it either.
+bool middle(int32_t rows, int32_t n)
+{
+    return rows > 64 && tiles_of(rows, n, 128, 128) >= kComputeUnits * 3 / 4;
+}
+uint32_t parts_of(int32_t rows, int32_t n, int32_t k)
+{
+    if (middle(rows, n)) return 1;
+    const int64_t fill = kComputeUnits / tiles_of(rows, n, 128, 64), most = blocks_of(k) / 6;
+    const int64_t parts = fill < most ? fill : most;
+    return parts < 2 ? 1 : (uint32_t)parts;
+}
+
+template <typename T, int NT, int AHEAD, bool GIVEN, bool GATED>
+hipError_t launch_few_form(const F8Args& a, hipStream_t s)
+{
+    const int blocks = blocks_of(a.k), waves = blocks < kMostWaves ? blocks : kMostWaves;
+    const int64_t tiles = ((int64_t)a.n + NT * 16 - 1) / (NT * 16);
+    return launch(few_kernel<T, NT, AHEAD, GIVEN, GATED>, dim3((unsigned)tiles),
+                  (unsigned)(waves * 64), 0, s, a, blocks);
 }
 
 template <typename T, bool GIVEN, bool GATED>
 hipError_t launch_few(const F8Args& a, hipStream_t s)
 {
-    if (a.rows <= 16) return launch_few_rows<T, 1, GIVEN, GATED>(a, s);
-    if (a.rows <= 32) return launch_few_rows<T, 2, GIVEN, GATED>(a, s);
-    return launch_few_rows<T, 4, GIVEN, GATED>(a, s);
+    if (a.n >= 64 * kComputeUnits) return launch_few_form<T, 4, 1, GIVEN, GATED>(a, s);
+    return launch_few_form<T, 1, 2, GIVEN, GATED>(a, s);
 }
 
-template <typename T, int WN, int WM, int TN, int TM, int STAGES, bool GATED, bool ALIGNED>
+template <typename T, int WN, int WM, int TN, int TM, int STAGES, bool SPLIT, bool GATED,
+          bool ALIGNED>
 hipError_t launch_tiles(const F8Args& a, Packed x, hipStream_t s)
 {
     constexpr int MB = WM * TM * 16, NB = WN * TN * 16, THREADS = WN * WM * 64;
-    const int64_t tiles_m = ((int64_t)a.rows + MB - 1) / MB;
-    const int64_t tiles = tiles_m * (((int64_t)a.n + NB - 1) / NB);
-    if (tiles > 0x7fffff00) return hipErrorInvalidConfiguration;
-    x.tiles_m = (uint32_t)tiles_m;
+    const int64_t tiles = tiles_of(a.rows, a.n, NB, MB);
+    x.tiles_m = (uint32_t)(((int64_t)a.rows + MB - 1) / MB);
     x.tiles = (uint32_t)tiles;
+    const int64_t all = tiles * x.parts, upto = (all + 7) / 8 * 8;
+    if (upto > 0x7fffffff) return hipErrorInvalidConfiguration;
     constexpr size_t lds = (size_t)STAGES * tile_stage(NB, MB);
     auto kernel = tile_kernel<T, WN, WM, TN, TM, STAGES, GATED, ALIGNED>;
     if (lds > 65536) {
@@ -640,28 +773,27 @@ hipError_t launch_tiles(const F8Args& a, Packed x, hipStream_t s)
                                                  (int)lds);
         if (e != hipSuccess) return e;
     }
-    const int64_t all = (tiles + 7) / 8 * 8, most = most_blocks(THREADS) / 8 * 8;
-    for (int64_t first = 0; first < all; first += most) {
+    const int64_t most = most_blocks(THREADS) / 8 * 8;
+    for (int64_t first = 0; first < upto; first += most) {
         x.first = (uint32_t)first;
-        const int64_t n = all - first < most ? all - first : most;
+        const int64_t n = upto - first < most ? upto - first : most;
         const hipError_t e = launch(kernel, dim3((unsigned)n), THREADS, lds, s, a, x);
         if (e != hipSuccess) return e;
     }
+    if constexpr (SPLIT)
+        if (x.parts > 1)
+            return launch(join_kernel<T, WN, WM, TN, TM, GATED>, dim3(x.tiles, TM), THREADS, 0, s, a, x);
     return hipSuccess;
 }
 
 template <typename T, bool GATED, bool ALIGNED>
 hipError_t launch_sizes(const F8Args& a, const Packed& x, hipStream_t s)
 {
-    auto tiles = [&](int n, int rows) {
-        return (((int64_t)a.rows + rows - 1) / rows) * (((int64_t)a.n + n - 1) / n);
-    };
     // registers hold no copy of unaligned weights beside the totals of a large tile
-    if (ALIGNED && tiles(256, 256) >= kComputeUnits / 2)
-        return launch_tiles<T, 4, 2, 4, 8, 2, GATED, true>(a, x, s);
-    if (tiles(128, 128) >= kComputeUnits * 3 / 4)
-        return launch_tiles<T, 2, 2, 4, 4, 3, GATED, ALIGNED>(a, x, s);
-    return launch_tiles<T, 4, 1, 2, 4, 4, GATED, ALIGNED>(a, x, s);
+    if (ALIGNED && tiles_of(a.rows, a.n, 256, 256) >= kComputeUnits / 2)
+        return launch_tiles<T, 4, 2, 4, 8, 2, false, GATED, true>(a, x, s);
+    if (middle(a.rows, a.n)) return launch_tiles<T, 2, 2, 4, 4, 3, false, GATED, ALIGNED>(a, x, s);
+    return launch_tiles<T, 4, 1, 2, 4, 4, true, GATED, ALIGNED>(a, x, s);
 }
 
 template <typename T, bool GATED>
@@ -669,8 +801,7 @@ hipError_t launch_many(const F8Args& a, hipStream_t s)
 {
     const int blocks = blocks_of(a.k);
     uint8_t* codes = static_cast<uint8_t*>(a.workspace);
-    const size_t size = ((size_t)a.rows * blocks * kBlock + 255) / 256 * 256;
-    float* scales = reinterpret_cast<float*>(codes + size);
+    float* scales = reinterpret_cast<float*>(codes + (size_t)a.rows * blocks * kBlock);
     const int64_t all = (int64_t)a.rows * blocks, most = most_blocks(256);
     hipError_t e;
     if (a.x_scales) {
@@ -684,16 +815,34 @@ hipError_t launch_many(const F8Args& a, hipStream_t s)
                    blocks);
     }
     if (e != hipSuccess) return e;
-    const Packed x = {codes, scales, blocks, 0, 0, 0};
-    const bool aligned = ((uintptr_t)a.codes | (uintptr_t)a.code_stride | (uintptr_t)a.k) % 16 == 0 &&
+    Packed x = {};
+    x.codes = codes;
+    x.scales = scales;
+    x.blocks = blocks;
+    x.parts = parts_of(a.rows, a.n, a.k);
+    x.join = reinterpret_cast<f32x4*>(codes + packed_bytes(a.rows, a.k));
+    const bool aligned = ((uintptr_t)a.codes | (uintptr_t)a.code_stride) % 16 == 0 &&
                          a.k % kBlock == 0;
     return aligned ? launch_sizes<T, GATED, true>(a, x, s) : launch_sizes<T, GATED, false>(a, x, s);
 }
 
+// Rows whose strides pass 2^28 go a few at a time.
 template <typename T>
 hipError_t launch_type(const F8Args& a, hipStream_t s)
 {
     const bool gated = a.act == RM_ACT_SWIGLU;
+    if (a.rows > kFewRows && few(a.rows, a.code_stride)) {
+        for (int32_t r = 0; r < a.rows; r += kFewRows) {
+            F8Args b = a;
+            b.rows = a.rows - r < kFewRows ? a.rows - r : kFewRows;
+            b.x = static_cast<const uint8_t*>(a.x) + r * a.x_stride * (a.x_scales ? 1 : 2);
+            if (a.x_scales) b.x_scales = a.x_scales + (int64_t)r * blocks_of(a.k);
+            b.y = static_cast<T*>(a.y) + r * a.y_stride;
+            const hipError_t e = launch_type<T>(b, s);
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    }
     if (!few(a.rows, a.code_stride)) return gated ? launch_many<T, true>(a, s) : launch_many<T, false>(a, s);
     if (a.x_scales) return gated ? launch_few<T, true, true>(a, s) : launch_few<T, true, false>(a, s);
     return gated ? launch_few<T, false, true>(a, s) : launch_few<T, false, false>(a, s);
@@ -714,10 +863,11 @@ hipError_t launch_quantize_type(int block_rows, const QuantizeArgs& a, hipStream
 
 size_t f8_workspace(int32_t rows, int32_t n, int32_t k, int32_t act)
 {
-    (void)n, (void)act;
+    (void)act;
     if (few(rows, 0)) return 0;
-    const size_t blocks = (size_t)blocks_of(k);
-    return ((size_t)rows * blocks * kBlock + 255) / 256 * 256 + (size_t)rows * blocks * 4;
+    const uint32_t parts = parts_of(rows, n, k);
+    const size_t join = parts > 1 ? (size_t)parts * tiles_of(rows, n, 128, 64) * 128 * 64 * 4 : 0;
+    return packed_bytes(rows, k) + join;
 }
 
 hipError_t launch_f8(int type, const F8Args& a, hipStream_t s)
