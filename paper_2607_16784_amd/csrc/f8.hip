@@ -16,6 +16,7 @@
 // both go through LDS, a step of 128 columns or more ahead.
 #include "rm_common.h"
 #include "rm_decode.h"
+#include "rm_lds.h"
 
 namespace rm {
 namespace {
@@ -419,33 +420,6 @@ struct Packed {
 // Bytes of a step in LDS: codes of the weights and of x, scales of x and 64 of the
 // weights (two a wave, and what the other lanes of their load bring).
 constexpr int tile_stage(int weights, int rows) { return (weights + rows) * kBlock + rows * 4 + 256; }
-
-// 16 bytes a lane from base + offset to LDS, lane by lane behind each other.  Not
-// the builtin: the compiler would wait for all of it before the next read of LDS.
-// m0 is a register that the compiler sets only beside its use.
-__device__ inline void to_lds16(uint32_t lds, uint32_t offset, const uint8_t* base)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                 :: "s"(lds), "v"(offset), "s"(base) : "memory");
-}
-// 4 bytes a lane from an address of its own.
-__device__ inline void to_lds4(uint32_t lds, const void* from)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
-                 :: "s"(lds), "v"(from) : "memory");
-}
-// An address that all lanes agree on, in scalar registers.
-__device__ inline const uint8_t* scalar(const uint8_t* p)
-{
-    const uint64_t v = (uint64_t)(uintptr_t)p;
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
-    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-    return (const uint8_t*)(uintptr_t)((uint64_t)hi << 32 | lo);
-}
-__device__ inline uint32_t lds_address(const void* p)
-{
-    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
-}
 
 // Bias, activation and the result of a wave's totals: outputs of tile `tile` of TN x 16
 // weight rows, rows of x from row0.

@@ -11,6 +11,7 @@
 // lane, so nothing but maxima and sums passes between lanes, and those between two.
 #include "rm_common.h"
 #include "rm_decode.h"
+#include "rm_lds.h"
 
 namespace rm {
 namespace {
@@ -167,12 +168,15 @@ struct PromptPlan {
     int64_t slots, clear, first;
 };
 
-template <typename T, int D>
-__global__ __launch_bounds__(kWaves * 64) void prompt_kernel(PromptArgs a, PromptPlan plan)
+// ALIGNED: keys and values by 16 bytes at addresses that are multiples of it, which go
+// to LDS directly; others go through registers.
+template <typename T, int D, bool ALIGNED>
+__global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(D <= 128 ? 2 : 1)))
+void prompt_kernel(PromptArgs a, PromptPlan plan)
 {
     typedef typename Vec<T>::x8 V;
     typedef typename Vec<T>::x2 V2;
-    constexpr int CHUNKS = D / 8, LOADS = kKeys * CHUNKS / (kWaves * 64);
+    constexpr int CHUNKS = D / 8, LOADS = kKeys * CHUNKS / (kWaves * 64), ROWS = 64 / CHUNKS;
     __shared__ __align__(1024) T keys[2][kKeys * D], values[2][kKeys * D];
 
     const int KV = a.kv_heads, G = a.heads / KV;
@@ -215,22 +219,40 @@ __global__ __launch_bounds__(kWaves * 64) void prompt_kernel(PromptArgs a, Promp
 
     const T* k_base = static_cast<const T*>(a.k) + begin * a.k_stride + head * a.k_head;
     const T* v_base = static_cast<const T*>(a.v) + begin * a.v_stride + head * a.v_head;
-    V kr[LOADS], vr[LOADS];
-    auto load = [&](int step) {
+    // Chunk c of a row lies at c with the row's bits in it (key_at, value_at), and a wave
+    // loads ROWS rows at a time.
+    const int row0 = wave * ROWS + lane / CHUNKS, chunk = lane % CHUNKS;
+    const uint32_t key_chunk = (chunk ^ (row0 & 7)) * 16, value_chunk = (chunk ^ (row0 & 3) * 2) * 16;
+    static_assert(ROWS * kWaves % 8 == 0, "the swapped chunks are those of every load");
+    const uint32_t k_row = (uint32_t)(a.k_stride * 2), v_row = (uint32_t)(a.v_stride * 2);
+    const uint32_t k_lds = __builtin_amdgcn_readfirstlane(lds_address(&keys[0][0]));
+    const uint32_t v_lds = __builtin_amdgcn_readfirstlane(lds_address(&values[0][0]));
+    V kr[ALIGNED ? 1 : LOADS], vr[ALIGNED ? 1 : LOADS];
+    auto load = [&](int step, int buffer) {
+        // behind the sequence's end its last row again, which the mask takes away
+        const int t0 = step * kKeys;
+        const uint32_t most = (uint32_t)(n - 1 - t0);
+        const T* kp = k_base + t0 * a.k_stride;
+        const T* vp = v_base + t0 * a.v_stride;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int c = i * kWaves * 64 + threadIdx.x;
-            const int64_t token = min(step * kKeys + c / CHUNKS, n - 1);
-            kr[i] = load8(k_base + token * a.k_stride + c % CHUNKS * 8);
-            vr[i] = load8(v_base + token * a.v_stride + c % CHUNKS * 8);
+            const uint32_t row = min((uint32_t)(row0 + i * ROWS * kWaves), most);
+            if (ALIGNED) {
+                const uint32_t to = buffer * (kKeys * D * 2) + (i * kWaves + wave) * 1024;
+                to_lds16(k_lds + to, row * k_row + key_chunk, scalar((const uint8_t*)kp));
+                to_lds16(v_lds + to, row * v_row + value_chunk, scalar((const uint8_t*)vp));
+            } else {
+                kr[ALIGNED ? 0 : i] = load8(kp + row * a.k_stride + key_chunk / 2);
+                vr[ALIGNED ? 0 : i] = load8(vp + row * a.v_stride + value_chunk / 2);
+            }
         }
     };
     auto store = [&](int buffer) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int c = i * kWaves * 64 + threadIdx.x, row = c / CHUNKS, chunk = c % CHUNKS;
-            *reinterpret_cast<V*>(&keys[buffer][key_at<D>(row, chunk)]) = kr[i];
-            *reinterpret_cast<V*>(&values[buffer][value_at<D>(row, chunk)]) = vr[i];
+        for (int i = 0; i < (ALIGNED ? 0 : LOADS); ++i) {
+            const int to = (i * kWaves + wave) * 512 + lane * 8;
+            *reinterpret_cast<V*>(&keys[buffer][to]) = kr[ALIGNED ? 0 : i];
+            *reinterpret_cast<V*>(&values[buffer][to]) = vr[ALIGNED ? 0 : i];
         }
     };
 
@@ -254,12 +276,13 @@ __global__ __launch_bounds__(kWaves * 64) void prompt_kernel(PromptArgs a, Promp
         for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
     float m = -INFINITY, l = 0.0f;
 
-    load(lo);
+    load(lo, lo & 1);
     for (int step = lo; step < hi; ++step) {
         const int buffer = step & 1, t0 = step * kKeys;
         store(buffer);
-        __syncthreads();
-        load(min(step + 1, hi - 1));
+        // the step's keys are there, and what the step before read is free
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (step + 1 < hi) load(step + 1, buffer ^ 1);
         if (t0 > wave_last || (a.window > 0 && t0 + kKeys <= wave_first - a.window + 1)) continue;
 
         f32x16 s[2];
@@ -385,25 +408,36 @@ PromptPlan plan_of(const PromptArgs& a)
     return p;
 }
 
-template <typename T, int D>
+template <typename T, int D, bool ALIGNED>
 hipError_t launch_form(const PromptArgs& a, hipStream_t s)
 {
     PromptPlan p = plan_of(a);
     const int64_t all = p.slots * a.kv_heads + p.clear, most = most_blocks(kWaves * 64) / 8 * 8;
     for (p.first = 0; p.first < all; p.first += most) {
         const int64_t n = all - p.first < most ? all - p.first : most;
-        const hipError_t e = launch(prompt_kernel<T, D>, dim3((unsigned)n), kWaves * 64, 0, s, a, p);
+        const hipError_t e = launch(prompt_kernel<T, D, ALIGNED>, dim3((unsigned)n), kWaves * 64, 0, s, a, p);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
 
+template <typename T, int D>
+hipError_t launch_width(const PromptArgs& a, hipStream_t s)
+{
+    const uint64_t bits = (uint64_t)(uintptr_t)a.k | (uint64_t)(uintptr_t)a.v |
+                          (uint64_t)(a.k_stride | a.k_head | a.v_stride | a.v_head) * 2;
+    // a step's rows are counted in 32 bits
+    const bool near = a.k_stride >= 0 && a.v_stride >= 0 && a.k_stride < 1 << 24 &&
+                      a.v_stride < 1 << 24;
+    return bits % 16 == 0 && near ? launch_form<T, D, true>(a, s) : launch_form<T, D, false>(a, s);
+}
+
 template <typename T>
 hipError_t launch_type(int head_dim, const PromptArgs& a, hipStream_t s)
 {
-    if (head_dim == 64) return launch_form<T, 64>(a, s);
-    if (head_dim == 128) return launch_form<T, 128>(a, s);
-    return launch_form<T, 256>(a, s);
+    if (head_dim == 64) return launch_width<T, 64>(a, s);
+    if (head_dim == 128) return launch_width<T, 128>(a, s);
+    return launch_width<T, 256>(a, s);
 }
 
 }  // namespace
