@@ -116,17 +116,22 @@ __device__ inline void clear_rows(const PromptArgs& a, int64_t group)
 }
 
 // A step's keys and values in LDS: rows of D channels, chunks of 16 bytes swapped
-// within a row so that the rows an access takes at once are spread over the banks:
-// eight keys, or four of the values.
+// within a row so that what an access takes at once is spread over the 64 banks: a
+// chunk of eight keys, or two pairs of chunks of four keys' values.
 template <int D>
 __device__ inline int key_at(int row, int chunk)
 {
     return row * D + (chunk ^ (row & 7)) * 8;
 }
 template <int D>
+__device__ inline int value_swap(int row)
+{
+    return (D == 64 ? row >> 1 & 1 : row & 3) * 4;
+}
+template <int D>
 __device__ inline int value_at(int row, int chunk)
 {
-    return row * D + (chunk ^ (row & 3) * 2) * 8;
+    return row * D + (chunk ^ value_swap<D>(row)) * 8;
 }
 
 // The operand of channels 32 d .. and the keys 16 t + 4 h + {0 .. 3, 8 .. 11} of the
@@ -165,7 +170,7 @@ __device__ inline bool any_odd(const T* values)
 }
 
 struct PromptPlan {
-    int64_t slots, clear, first;
+    uint32_t slots, first;       // of the tiles; the launch's first workgroup
 };
 
 // ALIGNED: keys and values by 16 bytes at addresses that are multiples of it, which go
@@ -180,12 +185,13 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
     __shared__ __align__(1024) T keys[2][kKeys * D], values[2][kKeys * D];
 
     const int KV = a.kv_heads, G = a.heads / KV;
-    const int64_t at = plan.first + blockIdx.x;
-    if (at >= plan.slots * KV) {
-        clear_rows<T, D>(a, at - plan.slots * KV);
+    const uint32_t at = plan.first + blockIdx.x;         // 31 bits (prompt_fits)
+    const uint32_t tiles = plan.slots * KV;
+    if (at >= tiles) {
+        clear_rows<T, D>(a, at - tiles);
         return;
     }
-    const int64_t slot = (uint64_t)at / (uint32_t)KV;
+    const uint32_t slot = at / (uint32_t)KV;
     const int head = (int)(at - slot * KV);
     const int b = sequence_at(a, G, slot);
     if (b < 0) return;
@@ -222,7 +228,7 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
     // Chunk c of a row lies at c with the row's bits in it (key_at, value_at), and a wave
     // loads ROWS rows at a time.
     const int row0 = wave * ROWS + lane / CHUNKS, chunk = lane % CHUNKS;
-    const uint32_t key_chunk = (chunk ^ (row0 & 7)) * 16, value_chunk = (chunk ^ (row0 & 3) * 2) * 16;
+    const uint32_t key_chunk = (chunk ^ (row0 & 7)) * 16, value_chunk = (chunk ^ value_swap<D>(row0)) * 16;
     static_assert(ROWS * kWaves % 8 == 0, "the swapped chunks are those of every load");
     const uint32_t k_row = (uint32_t)(a.k_stride * 2), v_row = (uint32_t)(a.v_stride * 2);
     const uint32_t k_lds = __builtin_amdgcn_readfirstlane(lds_address(&keys[0][0]));
@@ -256,14 +262,14 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
         }
     };
 
+    load(lo, lo & 1);
     V q[D / 16];
     {
         const T* row = static_cast<const T*>(a.q) + q_token * a.q_stride + q_head * a.q_head;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
             q[i] = load8(row + i * 16 + h * 8);
-            if (a.scale < 0) q[i] = -q[i];
-            if (a.scale == 0) q[i] = q[i] * (T)0.0f;
+            if (a.scale <= 0) q[i] = q[i] * (T)(a.scale < 0 ? -1.0f : 0.0f);
         }
     }
     // positive, so that the largest logit is that of the largest product, and so that
@@ -276,13 +282,34 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
         for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
     float m = -INFINITY, l = 0.0f;
 
-    load(lo, lo & 1);
     for (int step = lo; step < hi; ++step) {
         const int buffer = step & 1, t0 = step * kKeys;
         store(buffer);
         // the step's keys are there, and what the step before read is free
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (step + 1 < hi) load(step + 1, buffer ^ 1);
+        // 0 times a value that is not finite would reach rows that do not see it.  Where
+        // the mask cuts a step's keys and some value is not finite, the rows that see it
+        // get it here, and the product is without it.  Every wave finds the same.
+        const bool cut = t0 + kKeys - 1 > first_pos || (a.window > 0 && t0 <= last_pos - a.window);
+        if (cut && __any(any_odd<T, D>(values[buffer]))) {
+            for (int j = 0; j < kKeys; ++j) {
+                const int key = t0 + j;
+                if (key > pos || (a.window > 0 && key <= pos - a.window)) continue;
+#pragma unroll
+                for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int c = d * 32 + i / 4 * 8 + h * 4 + i % 4;
+                        const float v = (float)values[buffer][value_at<D>(j, c / 8) + c % 8];
+                        if (!(fabsf(v) < INFINITY)) o[d][i] += v;
+                    }
+            }
+            __syncthreads();
+            for (int i = threadIdx.x; i < kKeys * D; i += kWaves * 64)
+                if (!(fabsf((float)values[buffer][i]) < INFINITY)) values[buffer][i] = (T)0.0f;
+            __syncthreads();
+        }
         if (t0 > wave_last || (a.window > 0 && t0 + kKeys <= wave_first - a.window + 1)) continue;
 
         f32x16 s[2];
@@ -337,39 +364,10 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
                 l += e;
                 p[u * 2 + i / 8][i % 8] = (T)e;
             }
-        const T* tile_v = values[buffer];
-        const bool odd = masked && __any(any_odd<T, D>(tile_v));
-        if (odd) {
-            // 0 times a value that is not finite would reach rows that do not see it:
-            // those that do get it here, and the product is without it
-            for (int j = 0; j < kKeys; ++j) {
-                const int key = t0 + j;
-                if (key > pos || (a.window > 0 && key <= pos - a.window)) continue;
-#pragma unroll
-                for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int c = d * 32 + i / 4 * 8 + h * 4 + i % 4;
-                        const float v = (float)tile_v[value_at<D>(j, c / 8) + c % 8];
-                        if (!(fabsf(v) < INFINITY)) o[d][i] += v;
-                    }
-            }
-#pragma unroll
-            for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    V e = values_of<T, D>(tile_v, d, t);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (!(fabsf((float)e[i]) < INFINITY)) e[i] = (T)0.0f;
-                    o[d] = mfma(e, p[t], o[d]);
-                }
-            continue;
-        }
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) o[d] = mfma(values_of<T, D>(tile_v, d, t), p[t], o[d]);
+            for (int t = 0; t < 4; ++t) o[d] = mfma(values_of<T, D>(values[buffer], d, t), p[t], o[d]);
     }
     l = halves<Add>(l);
     const float inv = 1.0f / l;
@@ -398,23 +396,20 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
         }
 }
 
-PromptPlan plan_of(const PromptArgs& a)
+int64_t slots_of(const PromptArgs& a)
 {
-    PromptPlan p;
-    const int64_t group = a.heads / a.kv_heads;
-    p.slots = a.n_seqs ? (int64_t)a.n_tokens * group / kRows + a.n_seqs : 0;
-    p.clear = ((int64_t)a.n_tokens + kClear - 1) / kClear;
-    p.first = 0;
-    return p;
+    return a.n_seqs ? (int64_t)a.n_tokens * (a.heads / a.kv_heads) / kRows + a.n_seqs : 0;
 }
+int64_t clears_of(const PromptArgs& a) { return ((int64_t)a.n_tokens + kClear - 1) / kClear; }
 
 template <typename T, int D, bool ALIGNED>
 hipError_t launch_form(const PromptArgs& a, hipStream_t s)
 {
-    PromptPlan p = plan_of(a);
-    const int64_t all = p.slots * a.kv_heads + p.clear, most = most_blocks(kWaves * 64) / 8 * 8;
-    for (p.first = 0; p.first < all; p.first += most) {
-        const int64_t n = all - p.first < most ? all - p.first : most;
+    const int64_t slots = slots_of(a), all = slots * a.kv_heads + clears_of(a);
+    const int64_t most = most_blocks(kWaves * 64) / 8 * 8;
+    for (int64_t first = 0; first < all; first += most) {
+        const int64_t n = all - first < most ? all - first : most;
+        const PromptPlan p = {(uint32_t)slots, (uint32_t)first};
         const hipError_t e = launch(prompt_kernel<T, D, ALIGNED>, dim3((unsigned)n), kWaves * 64, 0, s, a, p);
         if (e != hipSuccess) return e;
     }
@@ -444,8 +439,7 @@ hipError_t launch_type(int head_dim, const PromptArgs& a, hipStream_t s)
 
 bool prompt_fits(const PromptArgs& a)
 {
-    const PromptPlan p = plan_of(a);
-    return p.slots * a.kv_heads + p.clear <= 0x7fffffff;
+    return slots_of(a) * a.kv_heads + clears_of(a) <= 0x7fffffff;
 }
 
 hipError_t launch_prompt(int type, int head_dim, const PromptArgs& a, hipStream_t s)
