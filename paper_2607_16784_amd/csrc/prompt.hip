@@ -67,20 +67,29 @@ __device__ inline int64_t first_slot(const PromptArgs& a, int group, int32_t off
     return (int64_t)row_of(a, offset) * group / kRows + b;
 }
 
-// The last sequence whose first slot is at most `slot`, -1 for none.
-__device__ inline int sequence_at(const PromptArgs& a, int group, int64_t slot)
+// The last sequence whose first slot is at most `slot`, with its borders; -1 for none.
+struct Found {
+    int sequence;
+    int32_t begin, end;
+};
+__device__ inline Found sequence_at(const PromptArgs& a, int group, int64_t slot)
 {
     const int lane = threadIdx.x & 63;
     int lo = 0, n = a.n_seqs;
     while (true) {
         const int step = (n + 63) / 64, b = lo + lane * step;
-        const bool before = lane * step < n &&
-                            first_slot(a, group, a.offsets[min(b, a.n_seqs - 1)], b) <= slot;
+        const int32_t offset = a.offsets[min(b, a.n_seqs)];
+        const bool before = lane * step < n && first_slot(a, group, offset, b) <= slot;
         const int hit = __popcll(__ballot(before)) - 1;
-        if (hit < 0) return -1;
+        if (hit < 0) return Found{-1, 0, 0};
         lo += hit * step;
         n = min(step, n - hit * step);
-        if (step == 1) return __builtin_amdgcn_readfirstlane(lo);
+        if (step > 1) continue;
+        lo = __builtin_amdgcn_readfirstlane(lo);
+        // the next lane has the end, mostly: a load less to wait for
+        const int at = __builtin_amdgcn_readfirstlane(hit);
+        return Found{lo, __builtin_amdgcn_readlane(offset, at),
+                     at < 63 ? __builtin_amdgcn_readlane(offset, at + 1) : a.offsets[lo + 1]};
     }
 }
 
@@ -193,10 +202,11 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
     }
     const uint32_t slot = at / (uint32_t)KV;
     const int head = (int)(at - slot * KV);
-    const int b = sequence_at(a, G, slot);
-    if (b < 0) return;
-    const int32_t begin = a.offsets[b], end = a.offsets[b + 1];
-    const int64_t count = (int64_t)end - begin, at_slot = slot - first_slot(a, G, begin, b);
+    const Found found = sequence_at(a, G, slot);
+    if (found.sequence < 0) return;
+    const int32_t begin = found.begin, end = found.end;
+    const int64_t count = (int64_t)end - begin;
+    const int64_t at_slot = slot - first_slot(a, G, begin, found.sequence);
     if (begin < 0 || end > a.n_tokens || count < 0 || count > a.max_tokens) {
         // its rows in range, a part each slot and head
         const int64_t lo = row_of(a, begin), rows = row_of(a, end) - lo;
@@ -312,6 +322,9 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
         }
         if (t0 > wave_last || (a.window > 0 && t0 + kKeys <= wave_first - a.window + 1)) continue;
 
+        // one wave's matrix instructions go before the other's softmax: 16 384 tokens of 32
+        // heads 2.05 ms, without 2.09
+        __builtin_amdgcn_s_setprio(1);
         f32x16 s[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -324,6 +337,7 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
                 s[u] = mfma(e, q[i], s[u]);
             }
         }
+        __builtin_amdgcn_s_setprio(0);
         // of register i of part u: key t0 + 32 u + 8 (i / 4) + 4 h + i % 4
         const bool masked = t0 + kKeys - 1 > wave_first ||
                             (a.window > 0 && t0 <= wave_last - a.window);
@@ -364,10 +378,12 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
                 l += e;
                 p[u * 2 + i / 8][i % 8] = (T)e;
             }
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
 #pragma unroll
             for (int t = 0; t < 4; ++t) o[d] = mfma(values_of<T, D>(values[buffer], d, t), p[t], o[d]);
+        __builtin_amdgcn_s_setprio(0);
     }
     l = halves<Add>(l);
     const float inv = 1.0f / l;
