@@ -699,16 +699,19 @@ int64_t tiles_of(int32_t rows, int32_t n, int weights, int height)
     return (((int64_t)rows + height - 1) / height) * (((int64_t)n + weights - 1) / weights);
 }
 
-// Tiles of 128 x 128 where they fill three quarters of the card; else of 128 x 64, their
-// columns in parts of 6 blocks or more where these do not fill it either.
-bool middle(int32_t rows, int32_t n)
+// Smaller tiles where larger ones leave a quarter of the card without any, and at last
+// their columns in parts of 6 blocks or more.  300 x 1024 x 4096: tiles of 128 weight
+// rows 18.0 us, of 64 16.3; 200 x 6144 x 4096 23.2 and 25.6.  40 x 2048 x 11008 took
+// 43 us without parts, 25 with them (tiles of 128).
+bool fills(int32_t rows, int32_t n, int weights, int height)
 {
-    return rows > 64 && tiles_of(rows, n, 128, 128) >= kComputeUnits * 3 / 4;
+    return tiles_of(rows, n, weights, height) >= kComputeUnits * 3 / 4;
 }
+bool middle(int32_t rows, int32_t n) { return rows > 64 && fills(rows, n, 128, 128); }
 uint32_t parts_of(int32_t rows, int32_t n, int32_t k)
 {
-    if (middle(rows, n)) return 1;
-    const int64_t fill = kComputeUnits / tiles_of(rows, n, 128, 64), most = blocks_of(k) / 6;
+    if (middle(rows, n) || fills(rows, n, 128, 64)) return 1;
+    const int64_t fill = kComputeUnits / tiles_of(rows, n, 64, 64), most = blocks_of(k) / 6;
     const int64_t parts = fill < most ? fill : most;
     return parts < 2 ? 1 : (uint32_t)parts;
 }
@@ -767,7 +770,9 @@ hipError_t launch_sizes(const F8Args& a, const Packed& x, hipStream_t s)
     if (ALIGNED && tiles_of(a.rows, a.n, 256, 256) >= kComputeUnits / 2)
         return launch_tiles<T, 4, 2, 4, 8, 2, false, GATED, true>(a, x, s);
     if (middle(a.rows, a.n)) return launch_tiles<T, 2, 2, 4, 4, 3, false, GATED, ALIGNED>(a, x, s);
-    return launch_tiles<T, 4, 1, 2, 4, 4, true, GATED, ALIGNED>(a, x, s);
+    if (fills(a.rows, a.n, 128, 64))
+        return launch_tiles<T, 4, 1, 2, 4, 3, false, GATED, ALIGNED>(a, x, s);
+    return launch_tiles<T, 2, 1, 2, 4, 3, true, GATED, ALIGNED>(a, x, s);
 }
 
 template <typename T, bool GATED>
@@ -840,7 +845,7 @@ size_t f8_workspace(int32_t rows, int32_t n, int32_t k, int32_t act)
     (void)act;
     if (few(rows, 0)) return 0;
     const uint32_t parts = parts_of(rows, n, k);
-    const size_t join = parts > 1 ? (size_t)parts * tiles_of(rows, n, 128, 64) * 128 * 64 * 4 : 0;
+    const size_t join = parts > 1 ? (size_t)parts * tiles_of(rows, n, 64, 64) * 64 * 64 * 4 : 0;
     return packed_bytes(rows, k) + join;
 }
 

@@ -91,7 +91,8 @@ SIZES = [(1, 1, 1), (1, 16, 128), (1, 130, 100), (2, 7, 129), (5, 1021, 515), (1
          (17, 100, 300), (33, 257, 640), (64, 300, 257), (64, 64, 4096), (65, 64, 128),
          (70, 250, 1000), (100, 513, 333), (129, 128, 128), (300, 300, 300), (513, 520, 264),
          (1, 17000, 128), (20, 33000, 64), (64, 33000, 130), (2, 40, 20000), (40, 100, 3000),
-         (17, 256, 2048), (300, 33000, 256), (100, 300, 12800)]
+         (17, 256, 2048), (300, 33000, 256), (100, 300, 12800), (60, 25000, 384),
+         (130, 13000, 256)]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
