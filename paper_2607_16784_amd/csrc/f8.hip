@@ -481,8 +481,8 @@ __device__ inline uint2 place_of(uint32_t tile, uint32_t tiles_n, uint32_t tiles
 // next step is there, and that one's weights and first rows are read beside the last
 // matrix instructions.  A product goes into its total kLag matrix instructions
 // behind its own, so that no vector instruction waits for one.
-// ALIGNED: weights by 16 bytes at addresses that are multiples of it, whole blocks;
-// they go to LDS directly, others through registers.
+// ALIGNED: weights by 16 bytes at addresses that are multiples of it; they go to LDS
+// directly, others through registers.
 template <typename T, int WN, int WM, int TN, int TM, int STAGES, bool GATED, bool ALIGNED>
 __global__ __launch_bounds__(WN * WM * 64) __attribute__((amdgpu_waves_per_eu(2))) void
 tile_kernel(F8Args a, Packed x)
@@ -547,9 +547,12 @@ tile_kernel(F8Args a, Packed x)
             to_lds16(to + X_AT + (i * WAVES + wave) * 1024, x_from[i], x_base + rows_at * kBlock);
         to_lds4(to + S_AT + wave * 64 % MB * 4, xs_base + rows_at);
         to_lds4(to + S_AT + MB * 4, ws_base + step);
+        // behind k the row's last codes again: x is 0 there, and a code that is NaN makes
+        // its row's results NaN anyhow
+        const uint32_t inside = (uint32_t)min(column, a.k - 16 - (int)c);
 #pragma unroll
         for (int i = 0; i < W_GROUPS; ++i) {
-            if (ALIGNED) to_lds16(to + (i * WAVES + wave) * 1024, w_from[i] + column, w_base[i] + c);
+            if (ALIGNED) to_lds16(to + (i * WAVES + wave) * 1024, w_from[i] + inside, w_base[i] + c);
             else kept[ALIGNED ? 0 : i] = load16_of(w_base[i] + w_from[i], c + column, a.k);
         }
     };
@@ -800,8 +803,7 @@ hipError_t launch_many(const F8Args& a, hipStream_t s)
     x.blocks = blocks;
     x.parts = parts_of(a.rows, a.n, a.k);
     x.join = reinterpret_cast<f32x4*>(codes + packed_bytes(a.rows, a.k));
-    const bool aligned = ((uintptr_t)a.codes | (uintptr_t)a.code_stride) % 16 == 0 &&
-                         a.k % kBlock == 0;
+    const bool aligned = ((uintptr_t)a.codes | (uintptr_t)a.code_stride | (uintptr_t)a.k) % 16 == 0;
     return aligned ? launch_sizes<T, GATED, true>(a, x, s) : launch_sizes<T, GATED, false>(a, x, s);
 }
 

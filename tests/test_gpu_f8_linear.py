@@ -92,7 +92,7 @@ SIZES = [(1, 1, 1), (1, 16, 128), (1, 130, 100), (2, 7, 129), (5, 1021, 515), (1
          (70, 250, 1000), (100, 513, 333), (129, 128, 128), (300, 300, 300), (513, 520, 264),
          (1, 17000, 128), (20, 33000, 64), (64, 33000, 130), (2, 40, 20000), (40, 100, 3000),
          (17, 256, 2048), (300, 33000, 256), (100, 300, 12800), (60, 25000, 384),
-         (130, 13000, 256)]
+         (130, 13000, 256), (90, 200, 16), (200, 300, 400), (40, 70, 3104), (270, 33000, 208)]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
@@ -132,6 +132,23 @@ def test_quantised_by_the_call_or_before_it(rows):
     y = api.rm_f8_linear(x, codes, scales)
     c, s = api.rm_f8_quantize(x)
     assert torch.equal(api.rm_f8_linear(c, codes, scales, x_scales=s, dtype=torch.float16), y)
+
+
+@pytest.mark.parametrize("rows", [3, 60, 200])
+@pytest.mark.parametrize("k", [400, 397, 384])
+def test_codes_that_are_nan_stay_in_their_rows(rows, k):
+    # rows of the weights behind each other: what is behind a row's end is the next's
+    codes, scales = weights(200, k, "none", 18)
+    x = normal((rows, k), 19, torch.bfloat16)
+    clean = api.rm_f8_linear(x, codes, scales)
+    bad = codes.clone()
+    bad.view(torch.uint8)[7, 0] = 0x7f
+    bad.view(torch.uint8)[90, k - 1] = 0xff
+    bad.view(torch.uint8)[199] = 0x7f
+    got = api.rm_f8_linear(x, bad, scales)
+    rest = [j for j in range(200) if j not in (7, 90, 199)]
+    assert torch.equal(got[:, rest], clean[:, rest])
+    assert torch.all(torch.isnan(got[:, [7, 90, 199]]))
 
 
 @pytest.mark.parametrize("rows", [2, 64, 100])
