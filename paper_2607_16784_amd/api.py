@@ -466,14 +466,15 @@ def _pitch(stride, rows, width, name):
     return stride
 
 
-def _apart(strides, shape, name):
-    """Strides of an output [tokens, heads, dim] whose rows may not overlap."""
-    (t, h, d), (ts, hs, _) = shape, strides
-    if (h <= 1 or hs >= d) and (t <= 1 or ts >= (h - 1) * hs * (h > 1) + d):
-        return strides
-    # heads in front of the tokens
-    if t > 1 and ts >= d and (h <= 1 or hs >= (t - 1) * ts + d):
-        return strides
+def _turned(out, like, dtype, shape, gpu, name):
+    """An output [tokens, heads, dim] and its strides; its rows may not overlap."""
+    t, h, d = shape
+    if out is None:
+        return like.new_empty(shape), (h * d, d)
+    ts, hs, _ = _rows(out, dtype, shape, gpu, name)
+    if ((h <= 1 or hs >= d) and (t <= 1 or ts >= (max(h, 1) - 1) * hs + d)) or \
+            (t > 1 and ts >= d and (h <= 1 or hs >= (t - 1) * ts + d)):    # heads in front
+        return out, (ts, hs)
     raise ValueError(f"{name}: rows overlap")
 
 
@@ -784,18 +785,16 @@ def rm_head_norm_rotary(q, k, inv_freq, positions=None, q_weight=None, k_weight=
     if q is not None:
         heads = q.shape[1]
         qs, qp = _rows(q, dtype, q.shape, gpu, "q"), q.data_ptr()
-        q_out = q.new_empty(q.shape) if q_out is None else q_out
-        qos, qo = _apart(_rows(q_out, dtype, q.shape, gpu, "q_out"), q.shape, "q_out"), \
-            q_out.data_ptr()
+        q_out, qos = _turned(q_out, q, dtype, q.shape, gpu, "q_out")
+        qo = q_out.data_ptr()
     if k is not None:
         if k.dim() != 3:
             raise ValueError("k: expected [tokens, kv_heads, head_dim]")
         kv_heads = k.shape[1]
         shape = (tokens, kv_heads, dim)
         ks, kp = _rows(k, dtype, shape, gpu, "k"), k.data_ptr()
-        k_out = k.new_empty(shape) if k_out is None else k_out
-        kos, ko = _apart(_rows(k_out, dtype, shape, gpu, "k_out"), shape, "k_out"), \
-            k_out.data_ptr()
+        k_out, kos = _turned(k_out, k, dtype, shape, gpu, "k_out")
+        ko = k_out.data_ptr()
     if (tokens | heads | kv_heads | dim) >> 31:
         _too_large("sizes", tokens, heads, kv_heads, dim)
     half = inv_freq.numel()
