@@ -48,6 +48,7 @@ CODES = {torch.int8: 0, torch.float8_e4m3fn: 1}
 ACT_NAMES = {"none": 0, "swiglu": 1}
 NORM_NAMES = {"rms": 0, "layer": 1}
 ROTARY_NAMES = {"half": 0, "interleaved": 1}
+F8_FEW_ROWS = 16      # that rm_f8_linear takes without a workspace
 
 
 class DeviceDesc(ctypes.Structure):
@@ -925,13 +926,15 @@ def rm_f8_linear(x, codes, scales, x_scales=None, bias=None, act="none", dtype=N
             code_pitch, _on_gpu(scales, torch.float32, (bands, blocks), gpu, "scales"),
             _on_gpu(bias, dtype, (n,), gpu, "bias"), act, out.data_ptr(), out_pitch)
     lib, stream = _lib or library(), _raw_stream(gpu)
-    if workspace is None:
-        code = lib.rm_f8_linear(*args, None, 0, stream)
-        if code == RM_EWORKSPACE:     # few rows need none, so it is asked for only then
-            workspace = torch.empty(lib.rm_f8_linear_workspace_bytes(rows, n, k, act),
-                                    dtype=torch.uint8, device=x.device)
     if workspace is not None:
-        code = lib.rm_f8_linear(*args, *_scratch(workspace, gpu), stream)
+        where, need = _scratch(workspace, gpu)
+    else:
+        where = None
+        need = rows > F8_FEW_ROWS and lib.rm_f8_linear_workspace_bytes(rows, n, k, act)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+            where = workspace.data_ptr()
+    code = lib.rm_f8_linear(*args, where, need, stream)
     if code:
         _check(code, "rm_f8_linear")
     return out

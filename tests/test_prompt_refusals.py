@@ -73,7 +73,8 @@ def test_f8(lib):
         assert lib.rm_f8_linear_workspace_bytes(s["rows"], s["n"], s["k"], 0) == 0
     need = lib.rm_f8_linear_workspace_bytes(500, 8, 64, 0)
     assert need >= 500 * (128 + 4)
-    assert lib.rm_f8_linear_workspace_bytes(16, 8, 64, 0) == 0
+    assert lib.rm_f8_linear_workspace_bytes(api.F8_FEW_ROWS, 1 << 20, 1 << 20, 0) == 0
+    assert lib.rm_f8_linear_workspace_bytes(api.F8_FEW_ROWS + 1, 8, 64, 0) > 0
     # few tiles: the columns' parts are in it
     assert lib.rm_f8_linear_workspace_bytes(64, 128, 12800, 0) >= 64 * 12800 + 16 * 64 * 128 * 4
     for kw in (dict(), dict(ws=P, size=need - 1), dict(ws=ctypes.c_void_p(257), size=need)):
