@@ -174,16 +174,18 @@ __device__ inline typename Vec<T>::x8 values_of(const T* values, int d, int t)
 template <typename T, int D>
 __device__ inline bool any_odd(const T* values)
 {
-    constexpr uint32_t top = Exponent<T>::bits;
-    bool odd = false;
-#pragma unroll 4
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 top = {0, 0};                  // of the magnitudes' bits, which are in their order
+#pragma unroll
     for (int i = 0; i < kKeys * D / 512; ++i) {
         const u32x4 v = reinterpret_cast<const u32x4*>(values)[i * 64 + (threadIdx.x & 63)];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            odd = odd || (v[j] & top) == top || (v[j] >> 16 & top) == top;
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t magnitude = v[j] & 0x7fff7fffu;
+            top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, magnitude));
+        }
     }
-    return odd;
+    return max(top[0], top[1]) >= Exponent<T>::bits;
 }
 
 struct PromptPlan {
