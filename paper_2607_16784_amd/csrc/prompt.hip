@@ -13,10 +13,10 @@
 // Bound by issue: a step of a wave is 1024 cycles of matrix instructions for heads of
 // 128 and about 900 of exponentials, sums and maxima.  32 rows a wave leave two waves
 // a SIMD (200 registers), one's products beside the other's softmax: 16 384 tokens of
-// 32 heads 2.05 ms (1070 TFLOP/s, the matrix cores busy for 51% of the cycles); with
+// 32 heads 2.04 ms (1080 TFLOP/s, the matrix cores busy for 51% of the cycles); with
 // keys and values staged in registers and one wave a SIMD 3.57 ms.  Heads of 64 have
-// half of the products beside the same softmax (8192 tokens 850 TFLOP/s); heads of 256
-// one wave a SIMD (610).
+// half of the products beside the same softmax (8192 tokens 900 TFLOP/s); heads of 256
+// one wave a SIMD (640).
 #include "rm_common.h"
 #include "rm_decode.h"
 #include "rm_lds.h"
@@ -170,7 +170,8 @@ __device__ inline typename Vec<T>::x8 values_of(const T* values, int d, int t)
                               (s16x8){x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]});
 }
 
-// Whether any of the step's values is not finite; each lane of a wave has a part.
+// Whether any of the step's values is not finite; each lane of a wave has a part.  By
+// the largest magnitude, without branches: 97 tokens 7.99 us, with one a value 9.65.
 template <typename T, int D>
 __device__ inline bool any_odd(const T* values)
 {

@@ -120,6 +120,28 @@ def test_on_another_stream():
     assert torch.equal(got, want)
 
 
+def test_two_calls_at_once():
+    # on two streams, again and again, without workspaces of the caller's
+    g = torch.Generator().manual_seed(10)
+    x = torch.randn((300, 640), generator=g).bfloat16().cuda()
+    w, s = api.rm_f8_quantize(torch.randn((900, 640), generator=g).bfloat16().cuda(), 128)
+    qkv = torch.randn((400, 8, 128), generator=g).bfloat16().cuda()
+    off = torch.tensor([0, 150, 400], dtype=torch.int32, device="cuda")
+
+    def calls():
+        return (api.rm_f8_linear(x, w, s), api.rm_f8_linear(x[:40], w, s),
+                api.rm_prompt_attention(qkv[:, :4], qkv[:, 4:6], qkv[:, 6:], off, 250))
+    want = calls()
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for turn in range(20):
+        with torch.cuda.stream(streams[turn % 2]):
+            got.append(calls())
+    torch.cuda.synchronize()
+    for turn, outs in enumerate(got):
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), turn
+
+
 def test_the_predictor_takes_prompts_and_steps():
     models = []
     for seed, (weights, head_norm) in enumerate(FORMS):
