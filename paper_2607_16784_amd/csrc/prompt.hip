@@ -20,6 +20,7 @@
 #include "rm_common.h"
 #include "rm_decode.h"
 #include "rm_lds.h"
+#include "rm_slots.h"
 
 namespace rm {
 namespace {
@@ -28,8 +29,9 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4;
-constexpr int kKeys = 64;                // a step
-constexpr int kRows = kWaves * 32;       // (token, head) pairs of a tile
+constexpr int kKeys = kStepKeys;
+constexpr int kRows = kTileRows;
+static_assert(kRows == kWaves * 32, "32 rows a wave");
 // Weights are 2^(logit - m) with m at most kSlack below the row's largest logit so
 // far (powers of two): m moves, and the sums with it, only where a logit passes it
 // by more, which after the first keys is seldom.  In f16 a weight of 2^kSlack times
@@ -63,31 +65,26 @@ __device__ inline float halves(float v)
     return Op::of(__builtin_bit_cast(float, h0), __builtin_bit_cast(float, h1));
 }
 
-// Tiles of the sequences lie in a row of slots, sequence b's from
-// floor(first row * group / kRows) + b on: that leaves each enough, whatever the
-// lengths, and the sequence of a slot is found by 64 lanes that ask at once.
-__device__ inline int32_t row_of(const PromptArgs& a, int32_t offset)
+__device__ inline SlotShape shape_of(const PromptArgs& a)
 {
-    return min(max(offset, 0), a.n_tokens);
-}
-__device__ inline int64_t first_slot(const PromptArgs& a, int group, int32_t offset, int b)
-{
-    return (int64_t)row_of(a, offset) * group / kRows + b;
+    return SlotShape{a.n_tokens, a.max_tokens, a.window, a.heads / a.kv_heads, a.kv_heads};
 }
 
-// The last sequence whose first slot is at most `slot`, with its borders; -1 for none.
+// The last sequence whose first slot is at most `slot`, found by 64 lanes that ask at
+// once, with its borders; -1 for none.  Where offsets decrease the lanes that say yes
+// are not the first ones, and it may be any sequence: tile_of takes what fits it.
 struct Found {
     int sequence;
     int32_t begin, end;
 };
-__device__ inline Found sequence_at(const PromptArgs& a, int group, int64_t slot)
+__device__ inline Found sequence_at(const PromptArgs& a, const SlotShape& shape, int64_t slot)
 {
     const int lane = threadIdx.x & 63;
     int lo = 0, n = a.n_seqs;
     while (true) {
         const int step = (n + 63) / 64, b = lo + lane * step;
         const int32_t offset = a.offsets[min(b, a.n_seqs)];
-        const bool before = lane * step < n && first_slot(a, group, offset, b) <= slot;
+        const bool before = lane * step < n && first_slot(shape, offset, b) <= slot;
         const int hit = __popcll(__ballot(before)) - 1;
         if (hit < 0) return Found{-1, 0, 0};
         lo += hit * step;
@@ -213,29 +210,18 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
     }
     const uint32_t slot = at / (uint32_t)KV;
     const int head = (int)(at - slot * KV);
-    const Found found = sequence_at(a, G, slot);
+    const SlotShape shape = shape_of(a);
+    const Found found = sequence_at(a, shape, slot);
     if (found.sequence < 0) return;
     const int32_t begin = found.begin, end = found.end;
-    const int64_t count = (int64_t)end - begin;
-    const int64_t at_slot = slot - first_slot(a, G, begin, found.sequence);
-    if (begin < 0 || end > a.n_tokens || count < 0 || count > a.max_tokens) {
-        // its rows in range, a part each slot and head
-        const int64_t lo = row_of(a, begin), rows = row_of(a, end) - lo;
-        const int64_t from = (at_slot * KV + head) * kRows / ((int64_t)KV * G);
-        const int64_t upto = ((at_slot * KV + head + 1) * kRows - 1) / ((int64_t)KV * G) + 1;
-        clear<T, D>(a, lo + min(from, rows), lo + min(upto, rows));
-        return;
-    }
-    // the last tiles take the longest, so they come first
-    const int64_t rows = count * G, tile = (rows + kRows - 1) / kRows - 1 - at_slot;
-    if (tile < 0) return;
+    const SlotTile tile = tile_of(shape, head, slot, found.sequence, begin, end);
+    if (tile.what == SlotTile::CLEAR) clear<T, D>(a, tile.clear_from, tile.clear_upto);
+    if (tile.what != SlotTile::ATTEND) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int li = lane & 31, h = lane >> 5;
-    const int n = (int)count, r0 = (int)(tile * kRows);
-    const int last_row = (int)min(rows, (tile + 1) * kRows) - 1;
+    const int n = end - begin, r0 = tile.first_row, last_row = tile.last_row;
     const int first_pos = r0 / G, last_pos = last_row / G;
-    const int lo = a.window > 0 ? max(0, first_pos - a.window + 1) / kKeys : 0;
-    const int hi = last_pos / kKeys + 1;
+    const int lo = tile.first_step, hi = tile.end_step;
     // of this wave's rows
     const int wave_r0 = r0 + wave * 32;
     const int wave_first = min(wave_r0, last_row) / G;
