@@ -288,6 +288,11 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
     float m = -INFINITY, l = 0.0f;
+    // whether the mask cuts the keys from t0 on, for some row of the tile
+    auto cut = [&](int t0) {
+        return t0 + kKeys - 1 > first_pos || (a.window > 0 && t0 <= last_pos - a.window);
+    };
+    bool odd = false;
 
     for (int step = lo; step < hi; ++step) {
         const int buffer = step & 1, t0 = step * kKeys;
@@ -296,22 +301,11 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (step + 1 < hi) load(step + 1, buffer ^ 1);
         // 0 times a value that is not finite would reach rows that do not see it.  Where
-        // the mask cuts a step's keys and some value is not finite, the rows that see it
-        // get it here, and the product is without it.  Every wave finds the same.
-        const bool cut = t0 + kKeys - 1 > first_pos || (a.window > 0 && t0 <= last_pos - a.window);
-        if (cut && __any(any_odd<T, D>(values[buffer]))) {
-            for (int j = 0; j < kKeys; ++j) {
-                const int key = t0 + j;
-                if (key > pos || (a.window > 0 && key <= pos - a.window)) continue;
-#pragma unroll
-                for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int c = d * 32 + i / 4 * 8 + h * 4 + i % 4;
-                        const float v = (float)values[buffer][value_at<D>(j, c / 8) + c % 8];
-                        if (!(fabsf(v) < INFINITY)) o[d][i] += v;
-                    }
-            }
+        // the mask cuts a step's keys and some value is not finite, the product is without
+        // it, and the rows that see it get it behind the last step.  Every wave finds the
+        // same.
+        if (cut(t0) && __builtin_expect(__any(any_odd<T, D>(values[buffer])), 0)) {
+            odd = true;
             __syncthreads();
             for (int i = threadIdx.x; i < kKeys * D; i += kWaves * 64)
                 if (!(fabsf((float)values[buffer][i]) < INFINITY)) values[buffer][i] = (T)0.0f;
@@ -384,6 +378,47 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
     }
     l = halves<Add>(l);
     const float inv = 1.0f / l;
+    if (__builtin_expect(odd, 0)) {
+        // Of the steps that are cut: what is not finite as it is, or NaN where its weight is
+        // 0 in the products' type.  Key by key, from memory: beside the last step's weights
+        // it would take registers from every step.
+        typedef T V4 __attribute__((ext_vector_type(4)));
+        typedef V4 V4u __attribute__((aligned(2)));
+        for (int key = lo * kKeys; key <= last_pos; ++key) {
+            if (key % kKeys == 0 && !cut(key)) {
+                key += kKeys - 1;
+                continue;
+            }
+            const T* v = v_base + key * a.v_stride + h * 4;
+            bool any = false;
+#pragma unroll
+            for (int c = 0; c < D; c += 8)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) any = any || !(fabsf((float)v[c + i]) < INFINITY);
+            if (!__any(any)) continue;
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                const V e = load8(k_base + key * a.k_stride + i * 16 + h * 8);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s = __builtin_fmaf((float)e[j], (float)q[i][j], s);
+            }
+            s = halves<Add>(s);
+            const float off = m == -INFINITY ? 0.0f : m - Lift<T>::power;
+            const T weight = (T)__builtin_amdgcn_exp2f(__builtin_fmaf(s, to_log2, -off));
+            if (key > pos || (a.window > 0 && key <= pos - a.window)) continue;
+#pragma unroll
+            for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const V4 four = *reinterpret_cast<const V4u*>(v + d * 32 + g * 8);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!(fabsf((float)four[i]) < INFINITY))
+                            o[d][g * 4 + i] += (float)weight > 0.0f ? (float)four[i] : __builtin_nanf("");
+                }
+        }
+    }
     T* out = static_cast<T*>(a.out) + (q_token * a.heads + q_head) * D;
     const bool mine_too = wave_r0 + li <= last_row;
 #pragma unroll
