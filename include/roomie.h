@@ -675,7 +675,8 @@ int rm_head_norm_rotary(int32_t type, int32_t n_tokens, int32_t heads, int32_t k
  * Strides in elements of tokens and heads, channels consecutive; out is dense.
  * head_dim 64, 128 or 256.  Logits, softmax statistics and sums are fp32; the
  * softmax weights enter the second product in q's type, 2^6 at most, relative to
- * one of the row's largest logits so far.  A row that t does not see does not
+ * one of the row's largest logits so far.  Sums stay within fp32 for values up to
+ * q's largest number.  A row that t does not see does not
  * reach it, whatever its keys and values hold.  An infinite value that t sees makes
  * that channel infinite, or NaN where its weight is 0 in q's type.
  * token_offsets may not decrease; where they do RM_ST_BAD_LENGTH is set and rows

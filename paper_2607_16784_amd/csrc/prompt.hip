@@ -32,15 +32,20 @@ constexpr int kWaves = 4;
 constexpr int kKeys = kStepKeys;
 constexpr int kRows = kTileRows;
 static_assert(kRows == kWaves * 32, "32 rows a wave");
-// Weights are 2^(logit - m) with m at most kSlack below the row's largest logit so
-// far (powers of two): m moves, and the sums with it, only where a logit passes it
-// by more, which after the first keys is seldom.  In f16 a weight of 2^kSlack times
-// 2^9 is within the type, and one of 2^-23 keeps all its bits.
+// Weights are 2^(logit - m + lift) with m at most kSlack below the row's largest logit
+// so far (powers of two): m moves, and the sums with it, only where a logit passes it
+// by more, which after the first keys is seldom.  In f16 the lift is 2^9: a weight of
+// 2^kSlack times it is within the type, and one of 2^-23 keeps all its bits.  In bf16
+// it takes the sum over all keys to 1/2 at most, so that no sum of weighted values
+// leaves fp32 where the values are near the largest number; what goes is the bits of
+// results below 2^-118 times the number of keys.
 constexpr float kSlack = 6.0f;
 
-template <typename T> struct Lift;
-template <> struct Lift<bf16> { static constexpr float power = 0.0f; };
-template <> struct Lift<f16> { static constexpr float power = 9.0f; };
+__device__ inline float lift_of(bf16, int keys) { return -(kSlack + 1 + (32 - __builtin_clz(keys))); }
+__device__ inline float lift_of(f16, int) { return 9.0f; }
+template <typename T> struct Largest;
+template <> struct Largest<bf16> { static constexpr float value = 0x1.fep127f; };
+template <> struct Largest<f16> { static constexpr float value = 65504.0f; };
 // the bits of the exponent, all of them set where a number is not finite
 template <typename T> struct Exponent;
 template <> struct Exponent<bf16> { static constexpr uint32_t bits = 0x7f80; };
@@ -287,7 +292,8 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
-    float m = -INFINITY, l = 0.0f;
+    const float lift = lift_of(T(), last_pos + 1);
+    float ref = -INFINITY, l = 0.0f;         // the row's m - lift, and its sum
     // whether the mask cuts the keys from t0 on, for some row of the tile
     auto cut = [&](int t0) {
         return t0 + kKeys - 1 > first_pos || (a.window > 0 && t0 <= last_pos - a.window);
@@ -347,19 +353,19 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
-        top = halves<Max>(top) * to_log2;
-        if (__any(top > m + kSlack)) {
+        top = halves<Max>(top) * to_log2 - lift;
+        if (__any(top > ref + kSlack)) {
             // rows that have seen nothing yet have sums of 0
-            const float to = fmaxf(m, top);
-            const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - to);
-            m = to;
+            const float to = fmaxf(ref, top);
+            const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - to);
+            ref = to;
             l *= f;
 #pragma unroll
             for (int d = 0; d < D / 32; ++d)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] *= f;
         }
-        const float off = m == -INFINITY ? 0.0f : m - Lift<T>::power;
+        const float off = ref == -INFINITY ? 0.0f : ref;
         V p[4];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
@@ -404,7 +410,7 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
                 for (int j = 0; j < 8; ++j) s = __builtin_fmaf((float)e[j], (float)q[i][j], s);
             }
             s = halves<Add>(s);
-            const float off = m == -INFINITY ? 0.0f : m - Lift<T>::power;
+            const float off = ref == -INFINITY ? 0.0f : ref;
             const T weight = (T)__builtin_amdgcn_exp2f(__builtin_fmaf(s, to_log2, -off));
             if (key > pos || (a.window > 0 && key <= pos - a.window)) continue;
 #pragma unroll
@@ -418,6 +424,21 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
                             o[d][g * 4 + i] += (float)weight > 0.0f ? (float)four[i] : __builtin_nanf("");
                 }
         }
+    }
+    // The sum has the weights before their rounding, so a mean of the largest numbers may
+    // come out beyond them.
+    float largest = 0.0f;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) largest = fmaxf(largest, fabsf(o[d][i]));
+    if (__builtin_expect(__any(largest * inv > Largest<T>::value), 0)) {
+        const float most = Largest<T>::value * l;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (fabsf(o[d][i]) < INFINITY) o[d][i] = fminf(fmaxf(o[d][i], -most), most);
     }
     T* out = static_cast<T*>(a.out) + (q_token * a.heads + q_head) * D;
     const bool mine_too = wave_r0 + li <= last_row;
