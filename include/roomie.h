@@ -683,9 +683,10 @@ int rm_head_norm_rotary(int32_t type, int32_t n_tokens, int32_t heads, int32_t k
  * of out are unspecified.  A sequence of more than max_tokens rows, or one that
  * leaves [0, n_tokens), sets RM_ST_BAD_LENGTH too, and its rows get 0.
  * Errors: RM_EINVAL (NULL pointer, negative size, heads not a multiple of
- *   kv_heads, scale not finite, window < 0, bad type), RM_EUNSUPPORTED (head_dim
- *   not listed, n_seqs over RM_MAX_SEQUENCES, heads over 65535, max_tokens *
- *   heads / kv_heads or the workgroups beyond 31 bits), RM_ELAUNCH.
+ *   kv_heads, scale or scale * log2(e) not finite, window < 0, bad type),
+ *   RM_EUNSUPPORTED (head_dim not listed, n_seqs over RM_MAX_SEQUENCES, heads over
+ *   65535, max_tokens * heads / kv_heads or the workgroups beyond 31 bits),
+ *   RM_ELAUNCH.
  */
 int rm_prompt_attention(int32_t type, int32_t n_tokens, int32_t heads, int32_t kv_heads,
                         int32_t head_dim, const void* q, int64_t q_stride, int64_t q_head_stride,

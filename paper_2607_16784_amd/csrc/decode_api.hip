@@ -276,7 +276,7 @@ int rm_prompt_attention(int32_t type, int32_t n_tokens, int32_t heads, int32_t k
                         void* out, int32_t* status, void* stream)
 {
     if (!rm::type_ok(type) || n_tokens < 0 || n_seqs < 0 || max_tokens < 0 || kv_heads < 1 ||
-        heads < 1 || heads % kv_heads || window < 0 || !std::isfinite(scale))
+        heads < 1 || heads % kv_heads || window < 0 || !std::isfinite(scale * rm::kLog2e))
         return RM_EINVAL;
     if (head_dim != 64 && head_dim != 128 && head_dim != 256) return RM_EUNSUPPORTED;
     if (n_seqs > RM_MAX_SEQUENCES || heads > 65535) return RM_EUNSUPPORTED;

@@ -286,7 +286,7 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
     }
     // positive, so that the largest logit is that of the largest product, and so that
     // what is masked stays -infinity
-    const float to_log2 = a.scale == 0 ? 1.0f : fabsf(a.scale) * 1.44269504088896340736f;
+    const float to_log2 = a.scale == 0 ? 1.0f : fabsf(a.scale) * kLog2e;
     f32x16 o[D / 32];
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)

@@ -249,6 +249,7 @@ struct PromptArgs {
     void* out;
     int32_t* status;
 };
+constexpr float kLog2e = 1.44269504088896340736f;
 // Whether the workgroups of a call can be counted in 31 bits.
 bool prompt_fits(const PromptArgs& a);
 hipError_t launch_prompt(int type, int head_dim, const PromptArgs& a, hipStream_t s);
