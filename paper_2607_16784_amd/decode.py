@@ -219,6 +219,8 @@ class DecodeModel:
         begins anew.  Returns [sum of lengths, width]."""
         if len(lengths) != state["table"].shape[0] or min(lengths, default=0) < 0:
             raise ValueError("lengths: expected a number of tokens for every sequence")
+        if x.shape != (sum(lengths), self.width):
+            raise ValueError(f"x: expected [{sum(lengths)}, {self.width}], got {list(x.shape)}")
         state["lengths"].copy_(torch.tensor(lengths, dtype=torch.int32))
         result = None
         for _, run in self.calls(x, state, lengths=lengths):
