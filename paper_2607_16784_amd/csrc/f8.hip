@@ -8,10 +8,13 @@
 // long as both operands keep it: lane l has the bytes 16 (l / 16) .. and
 // 64 + 16 (l / 16) .. of its row.
 //
-// Up to 16 rows of x (few_kernel): bound by reading the codes once.  The blocks go
-// round the waves of a workgroup, x is quantised in the registers of the wave that
-// multiplies it, and the waves' totals are joined through LDS.  One row of 4096 by
-// 4096 columns 6.2 us in a graph (2.7 TB/s), 16 by 28672 x 4096 33.5 us (3.5 TB/s).
+// Up to 16 rows of x (few_kernel): one row is bound by reading the codes, more also by
+// what every workgroup does again, reading and quantising x.  The blocks go round the
+// waves of a workgroup, x is quantised in the registers of the wave that multiplies it,
+// and the waves' totals are joined through LDS.  In a graph, with weights that come
+// from memory: 28672 x 4096 with 1 row 28.1 us (4.2 TB/s), 16 rows 32.1; 4096 x 4096
+// 7.2 and 8.6.  With the same weights again and again, which a cache of 256 MB then
+// holds: 20.9 and 26.3, 5.5 and 8.2; so are the figures beside the choices below.
 //
 // More (tile_kernel): x is quantised once into the workspace (4.7 to 5.4 TB/s for many
 // rows), then tiles of both go through LDS, a step of 128 columns or more ahead.  A
@@ -691,7 +694,10 @@ __global__ __launch_bounds__(WN * WM * 64) void join_kernel(F8Args a, Packed x)
 
 // ---- launches --------------------------------------------------------------
 
-constexpr int kFewRows = 16;       // the most rows that few_kernel takes
+// The most rows that few_kernel takes.  Weights from memory, 16 rows and 17 (tile_kernel):
+// 4096 x 4096 8.6 and 15.2 us, 28672 x 4096 32.1 and 36.2, 1022 x 5150 12.4 and 17.4,
+// 40960 x 4096 45.8 and 65.1.
+constexpr int kFewRows = 16;
 
 // tile_kernel counts the bytes of 8 rows of weights in 32 bits
 bool few(int32_t rows, int64_t code_stride) { return rows <= kFewRows || code_stride >= 1 << 28; }

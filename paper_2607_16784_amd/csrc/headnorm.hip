@@ -8,7 +8,9 @@
 // so gain, angle and rot_scale are one factor a channel, taken once a token and
 // side for all of a wave's heads.  Sines and cosines are taken once a token, a pair a
 // lane, and pass through LDS: each lane taking its own eight channels' took 8190 tokens
-// of 40 heads of 128 from 33 (5.1 TB/s) to 50 us.
+// of 40 heads of 128 from 33 (5.1 TB/s) to 50 us.  Halves of a `rot` that is no multiple
+// of 16 begin within another lane's chunk, and partners are read one by one: the same
+// tokens 66 (rot 72 and 120) to 76 us (36).
 #include "rm_decode.h"
 #include "rm_rotary.h"
 

@@ -10,13 +10,14 @@
 // four keys of one channel, is a transposing read of LDS.  Rows never leave their
 // lane, so nothing but maxima and sums passes between lanes, and those between two.
 //
-// Bound by issue: a step of a wave is 1024 cycles of matrix instructions for heads of
-// 128 and about 900 of exponentials, sums and maxima.  32 rows a wave leave two waves
-// a SIMD (200 registers), one's products beside the other's softmax: 16 384 tokens of
-// 32 heads 2.04 ms (1080 TFLOP/s, the matrix cores busy for 51% of the cycles); with
-// keys and values staged in registers and one wave a SIMD 3.57 ms.  Heads of 64 have
-// half of the products beside the same softmax (8192 tokens 900 TFLOP/s); heads of 256
-// one wave a SIMD (640).
+// A step of a wave is 1024 cycles of matrix instructions for heads of 128 and about 900
+// of exponentials, sums and maxima.  32 rows a wave leave two waves a SIMD (213
+// registers), but little of one's products falls beside the other's softmax: by the
+// counters both are 110% of the kernel's cycles.  16 384 tokens of 32 heads 2.03 to 2.16
+// ms from card to card (1080 to 1020 TFLOP/s, the matrix cores busy for 51 to 56% of the
+// cycles); with keys and values staged in registers and one wave a SIMD 3.57 ms.  Heads
+// of 64 have half of the products for the same softmax (8192 tokens of 32 heads 310 us,
+// 890 TFLOP/s); heads of 256 one wave a SIMD (8192 tokens of 16 heads 760 us, 720).
 #include "rm_common.h"
 #include "rm_decode.h"
 #include "rm_lds.h"
@@ -173,7 +174,7 @@ __device__ inline typename Vec<T>::x8 values_of(const T* values, int d, int t)
 }
 
 // Whether any of the step's values is not finite; each lane of a wave has a part.  By
-// the largest magnitude, without branches: 97 tokens 7.99 us, with one a value 9.65.
+// the largest magnitude: with a branch for each value 97 tokens took 1.7 us longer, of 8.
 template <typename T, int D>
 __device__ inline bool any_odd(const T* values)
 {
@@ -319,8 +320,8 @@ void prompt_kernel(PromptArgs a, PromptPlan plan)
         }
         if (t0 > wave_last || (a.window > 0 && t0 + kKeys <= wave_first - a.window + 1)) continue;
 
-        // one wave's matrix instructions go before the other's softmax: 16 384 tokens of 32
-        // heads 2.05 ms, without 2.09
+        // one wave's matrix instructions go before the other's softmax: without that 16 384
+        // tokens of 32 heads take 2% longer
         __builtin_amdgcn_s_setprio(1);
         f32x16 s[2];
 #pragma unroll

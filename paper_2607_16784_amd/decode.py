@@ -216,7 +216,9 @@ class DecodeModel:
 
     def prompt(self, x, state, lengths):
         """Whole prompts of lengths[b] tokens, behind each other in x: every sequence
-        begins anew.  Returns [sum of lengths, width]."""
+        begins anew.  Returns [sum of lengths, width].  The lengths are numbers of the
+        host, whose borders each call copies to the GPU: it cannot be captured, as a
+        step can."""
         if len(lengths) != state["table"].shape[0] or min(lengths, default=0) < 0:
             raise ValueError("lengths: expected a number of tokens for every sequence")
         if x.shape != (sum(lengths), self.width):
@@ -229,8 +231,9 @@ class DecodeModel:
 
 
 def trace(model, state, new=1, repeats=16, lengths=None):
-    """One step's kernels: a list of dicts name, grid, threads, regs, smem,
-    duration (microseconds); with `lengths` those of whole prompts.
+    """One step's launches of the library: a list of dicts name, grid, threads, regs,
+    smem, duration (microseconds); with `lengths` those of whole prompts.  What torch
+    launches for a step's positions is not among them.
 
     The step runs `repeats` times and each launch is timed in its place there, so
     its weights and its part of the cache come from where a step finds them; its
